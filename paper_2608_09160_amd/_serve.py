@@ -1,0 +1,184 @@
+"""ctypes binding of the attention block's entry points (include/qkn_rope.h, qkn_cache.h): argument marshalling
+only, as in ``_lib``.
+
+Row tensors are 2-D with a contiguous last dimension and any row stride; heads follow each other in a row, as
+the projection writes them. Each operator has a ``Prepared...`` class, whose arguments are checked and marshalled
+once (for serving loops and HIP graphs, the tensors stay referenced), and a function that makes the call at once.
+"""
+from __future__ import annotations
+
+import ctypes
+from dataclasses import dataclass
+from typing import Optional
+
+import torch
+
+from ._lib import _c_i64, _check, _f32, _rows, _stream, _vp, load as _load
+
+_int = ctypes.c_int
+
+
+class QknCache(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("num_pages", _c_i64),
+                ("page_size", ctypes.c_int32), ("n_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("fp8", ctypes.c_int32), ("k_page", _c_i64), ("k_head", _c_i64), ("k_token", _c_i64),
+                ("v_page", _c_i64), ("v_head", _c_i64), ("v_token", _c_i64)]
+
+
+class QknRopeScaling(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("base", "factor", "low", "high", "original", "magnitude")]
+
+
+class QknRopeSeg(ctypes.Structure):
+    _fields_ = [("x", _vp), ("ldx", _c_i64), ("w", _vp), ("partials", _vp), ("d_full", _c_i64), ("y", _vp),
+                ("ldy", _c_i64), ("heads", ctypes.c_int32)]
+
+
+def load() -> ctypes.CDLL:
+    """The library with these entry points' signatures declared."""
+    lib = _load()
+    if lib.qkn_rope_cache.argtypes is None:
+        lib.qkn_rope_table.argtypes = [_vp, _c_i64, _int, ctypes.POINTER(QknRopeScaling), _vp]
+        lib.qkn_rope_cache.argtypes = [ctypes.POINTER(QknRopeSeg), ctypes.POINTER(QknRopeSeg), _vp, _c_i64, _c_i64,
+                                       _int, _int, _int, _vp, _c_i64, _vp, _vp, ctypes.POINTER(QknCache), _int,
+                                       ctypes.c_float, _vp]
+    return lib
+
+
+_CACHE_DTYPES = {torch.bfloat16: 0, torch.float8_e4m3fn: 1, torch.uint8: 1}
+
+
+def _index(t: torch.Tensor, what: str, dtype: torch.dtype, numel: int) -> int:
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous {dtype} GPU tensor")
+    if t.numel() < numel:
+        raise ValueError(f"{what}: needs {numel} elements, has {t.numel()}")
+    return t.data_ptr()
+
+
+@dataclass
+class KVCache:
+    """Pools of pages [pages, kv heads, page size, head dim], of any strides with a contiguous last dimension
+    (a permuted view of another order works): bf16, or float8_e4m3fn (uint8 codes) with fp32 scales per KV head."""
+
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+
+    def struct(self) -> QknCache:
+        if self.k.dtype not in _CACHE_DTYPES or self.k.dtype != self.v.dtype:
+            raise TypeError(f"cache: expected two pools in bf16 or float8_e4m3fn, got {self.k.dtype}, {self.v.dtype}")
+        if self.k.dim() != 4 or self.k.shape != self.v.shape:
+            raise ValueError("cache: pools must be [pages, kv heads, page size, head dim], alike")
+        pages, n_kv, page, D = self.k.shape
+        strides = []
+        for name, t in (("k", self.k), ("v", self.v)):
+            if not t.is_cuda or (D > 1 and t.stride(3) != 1):
+                raise ValueError(f"cache.{name}: expected a GPU tensor with a contiguous last dimension")
+            # the stride of a dimension of one is never used
+            strides += [max(t.stride(i), D) if t.shape[i] == 1 else t.stride(i) for i in (0, 1, 2)]
+        return QknCache(self.k.data_ptr(), self.v.data_ptr(), _f32(self.k_scale, "k_scale", n_kv),
+                        _f32(self.v_scale, "v_scale", n_kv), pages, page, n_kv, D, _CACHE_DTYPES[self.k.dtype], *strides)
+
+
+@dataclass
+class RopeSeg:
+    """Q or K rows for the rotary pass; with w and partials (fp32 [tp, T]) the norm's Phases B+C come first."""
+
+    x: torch.Tensor                           # bf16 [T, heads * head_dim]
+    w: Optional[torch.Tensor] = None          # fp32 [heads * head_dim]
+    partials: Optional[torch.Tensor] = None   # fp32 [tp, T]
+    d_full: int = 0
+    y: Optional[torch.Tensor] = None          # bf16 [T, heads * head_dim]; Q's is allocated if None
+
+
+def qkn_rope_table(n_pos: int, rot_dim: int, base: float = 10000.0, factor: float = 1.0, low: float = 0.0,
+                   high: float = 0.0, original: float = 0.0, magnitude: float = 1.0,
+                   out: Optional[torch.Tensor] = None, device="cuda", stream=None) -> torch.Tensor:
+    """cos and sin of every position and pair, fp32 [n_pos, rot_dim / 2, 2]; see qkn_rope_scaling for the
+    scaling to long contexts."""
+    if out is None:
+        out = torch.empty(n_pos, max(rot_dim, 0) // 2, 2, dtype=torch.float32, device=device)
+    sc = QknRopeScaling(base, factor, low, high, original, magnitude)
+    _check(load().qkn_rope_table(_f32(out, "out", n_pos * (rot_dim // 2) * 2), n_pos, rot_dim, ctypes.byref(sc),
+                                 _stream(stream)), "qkn_rope_table")
+    return out
+
+
+class PreparedRopeCache:
+    """qkn_rope_cache with its arguments checked and marshalled once: Q and K rows (normalised first where a
+    segment has w) rotated by pos (int32 [T]) with table, Q to q.y, K to k.y where given, K and V to rows `slots`
+    (int64 [T], page * page size + row; negative: not cached) of the cache. table None: no rotation."""
+
+    def __init__(self, table: Optional[torch.Tensor], pos: Optional[torch.Tensor], head_dim: int,
+                 q: Optional[RopeSeg] = None, k: Optional[RopeSeg] = None, v: Optional[torch.Tensor] = None,
+                 cache: Optional[KVCache] = None, slots: Optional[torch.Tensor] = None, interleaved: bool = False,
+                 eps: float = 1e-6):
+        if q is None and k is None:
+            raise ValueError("q, k or both must be given")
+        T, tp, segs = None, None, []
+        for name, s in (("q", q), ("k", k)):
+            if s is None:
+                segs.append(None)
+                continue
+            px, ldx, Ts, width = _rows(s.x, f"{name}.x")
+            if width % head_dim:
+                raise ValueError(f"{name}.x: {width} columns are not whole heads of {head_dim}")
+            if T is not None and Ts != T:
+                raise ValueError("q and k must have the same number of tokens")
+            T = Ts
+            py, ldy = None, 0
+            if s.y is None and name == "q":
+                s.y = torch.empty((T, width), dtype=s.x.dtype, device=s.x.device)
+            if s.y is not None:
+                py, ldy, Ty, wy = _rows(s.y, f"{name}.y")
+                if (Ty, wy) != (T, width):
+                    raise ValueError(f"{name}.y: shape must match x")
+            pp = None
+            if s.w is not None:
+                if s.partials is None or s.partials.dim() != 2 or s.partials.shape[1] != T:
+                    raise ValueError(f"{name}.partials: expected [tp, {T}]")
+                if tp is not None and s.partials.shape[0] != tp:
+                    raise ValueError("q and k must have statistics of the same number of ranks")
+                tp = s.partials.shape[0]
+                pp = _f32(s.partials, f"{name}.partials")
+            segs.append(QknRopeSeg(px, ldx, _f32(s.w, f"{name}.w", width), pp, s.d_full, py, ldy, width // head_dim))
+        pv, ldv = None, 0
+        if v is not None:
+            pv, ldv, Tv, wv = _rows(v, "v")
+            if cache is None or (Tv, wv) != (T, cache.v.shape[1] * head_dim):
+                raise ValueError("v: expected a cache and rows of its heads, as many as q's and k's")
+        rot, n_pos, pt, pp = 0, 0, None, None
+        if table is not None:
+            if table.dim() != 3 or table.shape[2] != 2:
+                raise ValueError("table: expected [positions, rot_dim / 2, 2]")
+            n_pos, rot = table.shape[0], 2 * table.shape[1]
+            pt = _f32(table, "table")
+            if rot:
+                if pos is None:
+                    raise ValueError("pos: needed with a table")
+                pp = _index(pos, "pos", torch.int32, T)
+        ps = None
+        if cache is not None:
+            if slots is None:
+                raise ValueError("slots: needed with a cache")
+            ps = _index(slots, "slots", torch.int64, T)
+        self.q, self.k, self.v, self.cache = q, k, v, cache
+        self._keep = (table, pos, slots)
+        self._cache = cache.struct() if cache is not None else None
+        self._segs = segs
+        ref = [ctypes.byref(s) if s is not None else None for s in segs]
+        self._args = (ref[0], ref[1], pv, ldv, T, head_dim, rot, int(interleaved), pt, n_pos, pp, ps,
+                      ctypes.byref(self._cache) if cache is not None else None, tp or 1, ctypes.c_float(eps))
+        self._fn = load().qkn_rope_cache
+
+    def __call__(self, stream=None):
+        _check(self._fn(*self._args, _stream(stream)), "qkn_rope_cache")
+        return self.q.y if self.q is not None else None
+
+
+def qkn_rope_cache(table, pos, head_dim, q=None, k=None, v=None, cache=None, slots=None, interleaved=False,
+                   eps=1e-6, stream=None):
+    """PreparedRopeCache made and called once; returns q's rotated rows."""
+    return PreparedRopeCache(table, pos, head_dim, q, k, v, cache, slots, interleaved, eps)(stream)
