@@ -1,4 +1,4 @@
-"""ctypes binding of the attention block's entry points (include/qkn_rope.h, qkn_cache.h): argument marshalling
+"""ctypes binding of the attention block's entry points (include/qkn_rope.h, qkn_attn.h, qkn_cache.h): argument marshalling
 only, as in ``_lib``.
 
 Row tensors are 2-D with a contiguous last dimension and any row stride; heads follow each other in a row, as
@@ -34,6 +34,14 @@ class QknRopeSeg(ctypes.Structure):
                 ("ldy", _c_i64), ("heads", ctypes.c_int32)]
 
 
+class QknAttnArgs(ctypes.Structure):
+    _fields_ = [("q", _vp), ("ldq", _c_i64), ("out", _vp), ("ldo", _c_i64), ("lse", _vp), ("q_start", _vp),
+                ("kv_len", _vp), ("block_table", _vp), ("ld_table", _c_i64), ("T", _c_i64),
+                ("batch", ctypes.c_int32), ("n_q", ctypes.c_int32), ("max_q", ctypes.c_int32),
+                ("max_kv", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
 def load() -> ctypes.CDLL:
     """The library with these entry points' signatures declared."""
     lib = _load()
@@ -42,6 +50,9 @@ def load() -> ctypes.CDLL:
         lib.qkn_rope_cache.argtypes = [ctypes.POINTER(QknRopeSeg), ctypes.POINTER(QknRopeSeg), _vp, _c_i64, _c_i64,
                                        _int, _int, _int, _vp, _c_i64, _vp, _vp, ctypes.POINTER(QknCache), _int,
                                        ctypes.c_float, _vp]
+        lib.qkn_attn_workspace_bytes.argtypes = [ctypes.POINTER(QknAttnArgs), ctypes.POINTER(QknCache)]
+        lib.qkn_attn_workspace_bytes.restype = _c_i64
+        lib.qkn_attn.argtypes = [ctypes.POINTER(QknAttnArgs), ctypes.POINTER(QknCache), _vp, _c_i64, _vp]
     return lib
 
 
@@ -182,3 +193,72 @@ def qkn_rope_cache(table, pos, head_dim, q=None, k=None, v=None, cache=None, slo
                    eps=1e-6, stream=None):
     """PreparedRopeCache made and called once; returns q's rotated rows."""
     return PreparedRopeCache(table, pos, head_dim, q, k, v, cache, slots, interleaved, eps)(stream)
+
+
+def _workspace(workspace: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+    if workspace is None:
+        return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+    if workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace: expected a contiguous uint8 GPU tensor")
+    return workspace
+
+
+class PreparedAttn:
+    """qkn_attn with its arguments and workspace prepared once: attention of the new tokens q (bf16 [T, heads *
+    head_dim], the sequences in order) over the cache that holds their keys and values already.
+
+    block_table int32 [batch, pages of a sequence], q_start int32 [batch + 1], kv_len int32 [batch] (new tokens
+    included) are read by the kernel on the device: a replayed graph sees what they hold then. max_q and max_kv: the
+    largest numbers of new and cached tokens of a sequence (the default: T, and what block_table's rows can hold).
+    lse: optional fp32 [T, heads], receives the log-sum-exp. window: keys that a token sees, its own the last (0:
+    all)."""
+
+    def __init__(self, q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, q_start: torch.Tensor,
+                 kv_len: torch.Tensor, max_q: Optional[int] = None, max_kv: Optional[int] = None,
+                 scale: Optional[float] = None, causal: bool = True, window: int = 0,
+                 out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None):
+        c = cache.struct()
+        pq, ldq, T, width = _rows(q, "q")
+        if width % c.head_dim or (width // c.head_dim) % c.n_kv:
+            raise ValueError(f"q: {width} columns are not a multiple of {c.n_kv} heads of {c.head_dim}")
+        heads = width // c.head_dim
+        if out is None:
+            out = torch.empty((T, width), dtype=q.dtype, device=q.device)
+        po, ldo, To, wo = _rows(out, "out")
+        if (To, wo) != (T, width):
+            raise ValueError("out: shape must match q")
+        if block_table.dim() != 2:
+            raise ValueError("block_table: expected [batch, pages]")
+        batch, pages = block_table.shape
+        if q_start.numel() != batch + 1 or kv_len.numel() != batch:
+            raise ValueError(f"q_start, kv_len: expected {batch + 1} and {batch} elements")
+        if lse is not None and tuple(lse.shape) != (T, heads):
+            raise ValueError(f"lse: expected [{T}, {heads}]")
+        limit = 2 ** 31 - 1
+        max_q = min(T, limit) if max_q is None else max_q
+        max_kv = min(pages * c.page_size, limit) if max_kv is None else max_kv
+        a = QknAttnArgs(pq, ldq, po, ldo, _f32(lse, "lse"), _index(q_start, "q_start", torch.int32, batch + 1),
+                        _index(kv_len, "kv_len", torch.int32, batch),
+                        _index(block_table, "block_table", torch.int32, batch * pages), pages, T, batch, heads, max_q,
+                        max_kv, int(causal), window, c.head_dim ** -0.5 if scale is None else scale)
+        lib = load()
+        need = lib.qkn_attn_workspace_bytes(ctypes.byref(a), ctypes.byref(c))
+        if need < 0:
+            _check(int(need), "qkn_attn_workspace_bytes")
+        self.workspace = _workspace(workspace, need, q.device)
+        self.q, self.out, self.lse, self.cache = q, out, lse, cache
+        self._keep = (block_table, q_start, kv_len, a, c)
+        self._args = (ctypes.byref(a), ctypes.byref(c), self.workspace.data_ptr(), self.workspace.numel())
+        self._fn = lib.qkn_attn
+
+    def __call__(self, stream=None) -> torch.Tensor:
+        _check(self._fn(*self._args, _stream(stream)), "qkn_attn")
+        return self.out
+
+
+def qkn_attn(q, cache, block_table, q_start, kv_len, max_q=None, max_kv=None, scale=None, causal=True, window=0,
+             out=None, lse=None, workspace=None, stream=None) -> torch.Tensor:
+    """PreparedAttn made and called once."""
+    return PreparedAttn(q, cache, block_table, q_start, kv_len, max_q, max_kv, scale, causal, window, out, lse,
+                        workspace)(stream)

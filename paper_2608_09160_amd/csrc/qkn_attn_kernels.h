@@ -1,0 +1,659 @@
+// Attention over the paged cache: the kernels (templates; instantiated in qkn_attn_*.hip).
+//
+// Rows. The query heads of one KV head see the same keys, so a sequence's rows for KV head g are its (token, head of
+// the group) pairs, row r = token r / G, head g G + r % G: a tile of rows uses each key tile for all of them.
+//
+// Products (v_mfma_f32_16x16x32_bf16: A 16 x 32, B 32 x 16, lane l holds row (column) l mod 16, k 8 (l / 16) .. + 7;
+// result column l mod 16, rows 4 (l / 16) .. + 3). Scores are formed transposed, S^T = K Q^T: a lane then holds 4
+// keys of each 16 for one query row, its softmax needs no other lane, and its weights are, packed to bf16, already
+// the B operand of O^T = V^T P^T, with keys 16 a + 4 (l / 16) + r as the product's k (any order of keys serves, as
+// long as V's is the same). O^T also has one row per lane, so a row's rescaling is one factor per lane.
+// V^T is read from the row-major V tile by the transposing LDS read: 16 lanes fetch 4 rows (8 for FP8) of 16 columns
+// and lane i receives column i.
+//
+// Softmax. m is a bound on the row's scores that is raised only where a score exceeds it by 2^8 in weight
+// (`kSlack`): most tiles then need no maximum across lanes and no rescaling. Weights are at most 2^8, which changes
+// nothing in their relative rounding. The sum l is of the unrounded fp32 weights.
+//
+// Tiles. KT keys at a time, K and V rows straight from the cache's pages into LDS (buffer_load ... lds, 16 bytes a
+// lane), two buffers, the next tile in flight while one is computed. A wavefront fetches 16 rows at a time: they lie
+// in one page, whose descriptor ends at the sequence's last token (or has no bytes for a bad page number), so rows
+// past it read zeros. 16-byte chunks of a row are stored at chunk ^ f(row), f such that the rows of one LDS read
+// fall on different banks.
+//
+// Two ways to share the work of a workgroup:
+//   SHARED  every wavefront has its own 16 CB rows, all take the same key tiles (many rows: products bound it);
+//   !SHARED every wavefront takes its own key tiles for the same 16 CB rows, with no barrier in the loop, and the
+//           wavefronts' results are joined at the end (few rows: bytes bound it).
+// Over workgroups the keys are split further where rows alone do not fill the chip; qkn_attn_join adds the parts in
+// ascending order.
+#ifndef QKN_ATTN_KERNELS_H
+#define QKN_ATTN_KERNELS_H
+
+#include "qkn_block.h"
+
+namespace attn {
+
+using namespace qkn_block;
+
+typedef __amdgpu_buffer_rsrc_t Rsrc;
+typedef __attribute__((address_space(3))) unsigned char LdsByte;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+struct Pool {
+  const unsigned char* base;
+  const float* scale;
+  int64_t page, head;   // strides in bytes
+  uint32_t token;
+};
+
+struct Params {
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;
+  const int32_t* q_start;
+  const int32_t* kv_len;
+  const int32_t* table;
+  int64_t ldq, ldo, ld_table, T;
+  Pool k, v;
+  int64_t num_pages;
+  int32_t page_shift;
+  int32_t batch, n_q, n_kv, D, tiles;  // tiles: row tiles of the grid
+  int32_t causal, window;
+  float c;                             // scale * log2(e)
+  FastDiv group, kv_heads, splits;
+  // split keys: split s of row (t, h) at index (s T + t) n_q + h
+  float* part_o;                       // [splits, T * n_q, D]
+  f32x2* part_ml;                      // [splits, T * n_q]: bound (log2 units) and sum; sum 0: nothing
+  int32_t min_tiles;                   // key tiles of a split, at least
+};
+
+// A kernel and what its launch has to know.
+struct Variant {
+  const void* fn;
+  int rows, keys, threads, lds;  // rows of a workgroup; keys that its wavefronts take at a time, in all
+  const char* name;
+};
+
+constexpr float kSlack = 8.0f;  // log2
+constexpr float kLn2 = 0.693147180559945309f;
+
+__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
+
+__device__ __forceinline__ Rsrc rsrc(const void* base, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), static_cast<short>(0), static_cast<int>(bytes),
+                                           0x00020000);
+}
+// Lane l's 16 bytes at byte `off` of the buffer go to dst + 16 l.
+__device__ __forceinline__ void load_to_lds(Rsrc r, unsigned char* dst, uint32_t off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsByte*)dst, 16, off, 0, 0, 0);
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // all but the N youngest
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+__device__ __forceinline__ void group_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// DT: head size, rounded up (the rest reads as zeros); OCC: wavefronts per SIMD that the registers must allow.
+template <int DT_, bool FP8_, int CB_, int WAVES_, bool SHARED_, int KT_, int OCC_>
+struct Cfg {
+  static constexpr int DT = DT_, CB = CB_, WAVES = WAVES_, KT = KT_, OCC = OCC_;
+  static constexpr bool FP8 = FP8_, SHARED = SHARED_;
+  static constexpr int ES = FP8 ? 1 : 2;
+  static constexpr int RB = DT * ES;              // bytes of an LDS row
+  static constexpr int CH = RB / 16;              // its 16-byte chunks
+  static constexpr int RPL = 64 / CH;             // rows of one load instruction
+  static constexpr int PER256 = RB >= 256 ? 1 : 256 / RB;  // rows of one pass over the banks
+  static constexpr int BM = 16 * CB * (SHARED ? WAVES : 1);  // rows of a workgroup
+  static constexpr int TILE = KT * RB;            // bytes of a K (V) tile
+  static constexpr int BLOCKS = SHARED ? KT / 16 / WAVES : KT / 16;  // 16-row blocks that a wavefront loads
+  static constexpr int LOADS = 2 * BLOCKS * 16 / RPL;  // load instructions of a wavefront per tile
+  static constexpr int STAGES = SHARED ? 1 : WAVES;    // key streams of a workgroup
+  static constexpr int JOIN_ROW = DT + 4;         // floats of a row while wavefronts are joined
+  static constexpr int JOIN = SHARED ? 0 : WAVES * 16 * CB * (JOIN_ROW + 2) * 4;
+  static constexpr int LDS = 4 * TILE * STAGES > JOIN ? 4 * TILE * STAGES : JOIN;
+  static_assert(!SHARED || KT == 16 * WAVES, "a block of 16 rows for every wavefront");
+  static_assert(LDS <= 160 * 1024, "LDS");
+  static_assert(CH <= 64 && LOADS < 64, "loads");
+  // Chunk c of row r is stored at c ^ swizzle(r). K: 16 lanes read the same chunk of 16 rows.
+  __device__ static constexpr int swizzle_k(int r) { return (r / PER256) & ((CH < 16 ? CH : 16) - 1); }
+  // V, bf16: 32 lanes read 2 chunks of 8 rows. FP8: one chunk of rows 0 to 7 and 16 to 23.
+  __device__ static constexpr int swizzle_v(int r) {
+    if constexpr (FP8) return ((r & 7) / PER256) | (((r >> 4) & 1) * (8 / PER256));
+    else return (((r & 7) / PER256) * 2) & (CH - 1);
+  }
+};
+
+// The keys that the workgroup's (wavefront's) rows see.
+struct Range {
+  int32_t lo, hi;
+};
+
+template <class C>
+struct Tiles {
+  // One wavefront's view of the key tiles: which lane fetches and reads what.
+  unsigned char* buf;       // its stream's two buffers: K, V, K, V
+  int lane, wave;
+  const Params& p;
+  int64_t head_k, head_v;   // bytes to the head
+  int32_t kv_len;
+  const int32_t* table;     // the sequence's pages
+  int32_t last_page;        // last entry in use
+  int32_t page0;            // pages held: lane i has entry page0 + i, then page0 + 64 + i
+  int32_t cur, next;
+
+  __device__ __forceinline__ Tiles(const Params& pp, unsigned char* b, int l, int w) : buf(b), lane(l), wave(w), p(pp) {}
+
+  __device__ __forceinline__ int32_t entry(int32_t i) const {
+    i = i < last_page ? i : last_page;
+    return table[i < 0 ? 0 : i];
+  }
+  __device__ __forceinline__ void open(int b, int head, int32_t m, int32_t first_key) {
+    head_k = head * p.k.head;
+    head_v = head * p.v.head;
+    kv_len = m;
+    table = p.table + b * p.ld_table;
+    last_page = (m - 1) >> p.page_shift;
+    page0 = first_key >> p.page_shift;
+    cur = entry(page0 + lane);
+    next = entry(page0 + 64 + lane);
+  }
+  // Requests rows [j0, j0 + KT) (SHARED: this wavefront's 16 of them) into buffer `at`.
+  __device__ __forceinline__ void request(int32_t j0, int at) {
+    unsigned char* kbuf = buf + at * 2 * C::TILE;
+#pragma unroll
+    for (int bl = 0; bl < C::BLOCKS; ++bl) {
+      const int blk = C::SHARED ? wave : bl;
+      const int32_t j = j0 + 16 * blk;
+      const int32_t pi = j >> p.page_shift;
+      while (pi - page0 >= 64) {  // pages are taken in ascending order
+        cur = next;
+        page0 += 64;
+        next = entry(page0 + 64 + lane);
+      }
+      const int32_t page = __builtin_amdgcn_readlane(cur, pi - page0);
+      const int32_t row0 = j & ((1 << p.page_shift) - 1);
+      const int32_t left = kv_len - j;
+      const uint32_t rows = left < 0 || static_cast<uint32_t>(page) >= p.num_pages ? 0 : left < 16 ? left : 16;
+      const uint32_t k_bytes = rows ? (rows - 1) * p.k.token + p.D * C::ES : 0;
+      const uint32_t v_bytes = rows ? (rows - 1) * p.v.token + p.D * C::ES : 0;
+      const int64_t pg = rows ? page : 0;
+      const Rsrc rk = rsrc(p.k.base + pg * p.k.page + head_k + static_cast<int64_t>(row0) * p.k.token, k_bytes);
+      const Rsrc rv = rsrc(p.v.base + pg * p.v.page + head_v + static_cast<int64_t>(row0) * p.v.token, v_bytes);
+#pragma unroll
+      for (int i = 0; i < 16 / C::RPL; ++i) {
+        const int r = i * C::RPL + lane / C::CH;
+        const int ck = (lane % C::CH) ^ C::swizzle_k(r), cv = (lane % C::CH) ^ C::swizzle_v(r + 16 * blk);
+        unsigned char* dst = kbuf + (16 * blk + i * C::RPL) * C::RB;
+        load_to_lds(rk, dst, ck * 16 < p.D * C::ES ? r * p.k.token + ck * 16 : 0x7fffffffu);
+        load_to_lds(rv, dst + C::TILE, cv * 16 < p.D * C::ES ? r * p.v.token + cv * 16 : 0x7fffffffu);
+      }
+    }
+  }
+  // A weight of 0 times an infinite or NaN value is NaN, which a row that does not see the key must not get. In a
+  // tile that some rows see in part the product takes 0 in the place of such values (add_infinities gives them to the
+  // rows that see them): puts it there in the V rows that this wavefront fetched; true if it found any.
+  __device__ __forceinline__ bool make_finite(int at) {
+    bool any = false;
+#pragma unroll
+    for (int bl = 0; bl < C::BLOCKS; ++bl)
+#pragma unroll
+      for (int i = 0; i < 16 / C::RPL; ++i) {
+        const int blk = C::SHARED ? wave : bl;
+        u32x4* src = reinterpret_cast<u32x4*>(buf + at * 2 * C::TILE + C::TILE + (16 * blk + i * C::RPL) * C::RB + lane * 16);
+        u32x4 u = *src;
+        bool bad = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t field = C::FP8 ? 0x7fu : 0x7f80u;  // all ones: NaN; infinite or NaN
+#pragma unroll
+          for (int h = 0; h < 32; h += C::FP8 ? 8 : 16)
+            if (((u[e] >> h) & field) == field) {
+              u[e] &= ~((C::FP8 ? 0xffu : 0xffffu) << h);
+              bad = true;
+            }
+        }
+        if (__builtin_amdgcn_ballot_w64(bad)) {
+          *src = u;
+          any = true;
+        }
+      }
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): written before the barrier
+    return any;
+  }
+  // A operand of S^T: 16 keys from row 16 kb, elements 32 step .. + 31.
+  __device__ __forceinline__ bf16x8 k_frag(int at, int kb, int step) const {
+    const int r = lane & 15, g = lane >> 4;
+    const unsigned char* row = buf + at * 2 * C::TILE + (16 * kb + r) * C::RB;
+    if constexpr (C::FP8) {
+      const int c = 2 * step + (g >> 1);
+      return widen(*reinterpret_cast<const i32x2*>(row + ((c ^ C::swizzle_k(r)) * 16) + (g & 1) * 8));
+    } else {
+      const int c = 4 * step + g;
+      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(row + (c ^ C::swizzle_k(r)) * 16));
+    }
+  }
+  // A operand of O^T: elements 16 db .. + 15 of 32 keys from row 32 kc; k slot 8 g + e is key 4 g + e (e < 4), or
+  // 16 + 4 g + e - 4.
+  __device__ __forceinline__ bf16x8 v_frag(int at, int kc, int db) const {
+    const int i = lane & 15, g = lane >> 4;
+    unsigned char* tile = buf + at * 2 * C::TILE + C::TILE + 32 * kc * C::RB;
+    if constexpr (C::FP8) {
+      const int j = i >> 1, r = j < 4 ? 4 * g + j : 12 + 4 * g + j;
+      unsigned char* src = tile + r * C::RB + (db ^ C::swizzle_v(r)) * 16 + (i & 1) * 8;
+      return widen(__builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(src)));
+    } else {
+      const int r = 4 * g + (i >> 2);
+      unsigned char* src = tile + r * C::RB + ((2 * db + ((i >> 1) & 1)) ^ C::swizzle_v(r)) * 16 + (i & 1) * 8;
+      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src));
+      const s16x4 b =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src + 16 * C::RB));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+  // Eight e4m3fn codes as bf16, exactly.
+  __device__ static __forceinline__ bf16x8 widen(i32x2 w) {
+    bf16x8 f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], 1.0f, false);
+      const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], 1.0f, true);
+      f[4 * e] = lo[0];
+      f[4 * e + 1] = lo[1];
+      f[4 * e + 2] = hi[0];
+      f[4 * e + 3] = hi[1];
+    }
+    return f;
+  }
+};
+
+// Running state of a wavefront's 16 CB rows: column block cb, this lane's row 16 cb + lane % 16.
+template <class C>
+struct Rows {
+  bf16x8 q[C::DT / 32][C::CB];
+  f32x4 o[C::DT / 16][C::CB];   // O^T, this lane's elements 16 db + 4 (lane / 16) .. + 3
+  float m[C::CB], l[C::CB];     // bound (of raw scores); sum over this lane's keys
+  int32_t lo[C::CB], hi[C::CB]; // the keys that the row sees
+};
+
+// One tile of keys j0 .. j0 + KT - 1 for one wavefront's rows. masked: some row does not see some of them.
+template <class C>
+__device__ __forceinline__ void tile_step(const Tiles<C>& t, Rows<C>& w, int at, int32_t j0, float c, bool masked) {
+  constexpr int KB = C::KT / 16, KC = C::KT / 32, ND = C::DT / 16, NS = C::DT / 32;
+  const int g = t.lane >> 4;
+  f32x4 s[KB][C::CB];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int cb = 0; cb < C::CB; ++cb) s[kb][cb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  // one operand ahead of the products, no more: left to itself the compiler reads them all first and runs out of
+  // registers
+  bf16x8 a[2];
+  a[0] = t.k_frag(at, 0, 0);
+#pragma unroll
+  for (int i = 0; i < NS * KB; ++i) {
+    const int step = i / KB, kb = i % KB;
+    if (i + 1 < NS * KB) a[(i + 1) & 1] = t.k_frag(at, (i + 1) % KB, (i + 1) / KB);
+#pragma unroll
+    for (int cb = 0; cb < C::CB; ++cb)
+      s[kb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i & 1], w.q[step][cb], s[kb][cb], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
+  if (masked) {
+#pragma unroll
+    for (int cb = 0; cb < C::CB; ++cb) {
+      const uint32_t seen = static_cast<uint32_t>(w.hi[cb] - w.lo[cb]);
+      const int32_t first = j0 + 4 * g - w.lo[cb];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          s[kb][cb][r] = static_cast<uint32_t>(first + 16 * kb + r) < seen ? s[kb][cb][r] : neg_inf();
+    }
+  }
+  // the largest score of this lane's keys against the row's bound
+  bool raise = false;
+  float top[C::CB];
+#pragma unroll
+  for (int cb = 0; cb < C::CB; ++cb) {
+    float x = s[0][cb][0];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x = fmaxf(x, s[kb][cb][r]);
+    top[cb] = x;
+    raise |= (x - w.m[cb]) * c > kSlack;  // m = -infinity: any score (+infinity), or none (NaN: false)
+  }
+  if (__builtin_amdgcn_ballot_w64(raise)) {
+#pragma unroll
+    for (int cb = 0; cb < C::CB; ++cb) {
+      float x = fmaxf(top[cb], w.m[cb]);
+      x = fmaxf(x, __shfl_xor(x, 16));
+      x = fmaxf(x, __shfl_xor(x, 32));
+      // each row for itself, so that a row's result does not depend on what else is in the wavefront
+      const bool raised = (x - w.m[cb]) * c > kSlack;
+      const float f = raised ? __builtin_amdgcn_exp2f((w.m[cb] - x) * c) : 1.0f;
+      w.m[cb] = raised ? x : w.m[cb];
+      w.l[cb] *= f;
+#pragma unroll
+      for (int db = 0; db < ND; ++db)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) w.o[db][cb][r] *= f;
+    }
+  }
+
+  // weights, their sums, and the operand of the second product
+  bf16x8 pf[KC][C::CB];
+#pragma unroll
+  for (int cb = 0; cb < C::CB; ++cb) {
+    const float shift = w.m[cb] == neg_inf() ? 0.0f : -w.m[cb] * c;
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * kc + e / 4][cb][e % 4], c, shift));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * kc + e / 4][cb][e % 4 + 1], c, shift));
+        w.l[cb] += p0;
+        w.l[cb] += p1;
+        const bf16x2 pk = __builtin_convertvector(f32x2{p0, p1}, bf16x2);
+        pf[kc][cb][e] = pk[0];
+        pf[kc][cb][e + 1] = pk[1];
+      }
+  }
+
+  a[0] = t.v_frag(at, 0, 0);
+#pragma unroll
+  for (int i = 0; i < KC * ND; ++i) {
+    const int kc = i / ND, db = i % ND;
+    if (i + 1 < KC * ND) a[(i + 1) & 1] = t.v_frag(at, (i + 1) / ND, (i + 1) % ND);
+#pragma unroll
+    for (int cb = 0; cb < C::CB; ++cb)
+      w.o[db][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i & 1], pf[kc][cb], w.o[db][cb], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// The infinite and NaN values of a masked tile, which its product left out, for the rows that see them.
+template <class C>
+__device__ __forceinline__ void add_infinities(const Tiles<C>& t, Rows<C>& w, int32_t j0) {
+#pragma unroll 1
+  for (int32_t j = j0; j < j0 + C::KT && j < t.kv_len; ++j) {
+    const int64_t page = t.table[j >> t.p.page_shift];
+    if (page < 0 || page >= t.p.num_pages) continue;
+    const unsigned char* row =
+        t.p.v.base + page * t.p.v.page + t.head_v + (j & ((1 << t.p.page_shift) - 1)) * static_cast<int64_t>(t.p.v.token);
+#pragma unroll
+    for (int db = 0; db < C::DT / 16; ++db) {
+      const int d = 16 * db + 4 * (t.lane >> 4);
+      if (d >= t.p.D) continue;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float v;
+        if constexpr (C::FP8) v = (row[d + r] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f;
+        else v = bf16_lo(reinterpret_cast<const uint16_t*>(row)[d + r]);
+        if (__builtin_isfinite(v)) continue;
+#pragma unroll
+        for (int cb = 0; cb < C::CB; ++cb)
+          if (j >= w.lo[cb] && j < w.hi[cb]) w.o[db][cb][r] += v;
+      }
+    }
+  }
+}
+
+// The sequence that row tile `idx` of the grid belongs to. Sequence b's tiles begin at q_start[b] G / BM + b: that
+// leaves each at least the tiles it needs. 64 lanes probe at once: one round for up to 64 sequences.
+template <int BM>
+__device__ __forceinline__ int find_sequence(const Params& p, int lane, int32_t idx) {
+  int lo = 0;
+  int64_t step = 1;
+  while (step * 64 < p.batch) step *= 64;
+  for (; step > 0; step /= 64) {
+    const int64_t b = lo + lane * step;
+    bool before = false;
+    if (b < p.batch) {
+      int32_t q0 = p.q_start[b];
+      q0 = q0 < 0 ? 0 : q0 > p.T ? static_cast<int32_t>(p.T) : q0;
+      before = static_cast<int64_t>(q0) * p.group.d / BM + b <= idx;
+    }
+    const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(before));
+    lo += static_cast<int>((n ? n - 1 : 0) * step);
+  }
+  return lo;
+}
+
+template <class C>
+__global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const Params p) {
+  __shared__ __align__(16) unsigned char lds[C::LDS];
+  __shared__ int any_infinite;
+  constexpr int ND = C::DT / 16, NS = C::DT / 32;
+  const int lane = static_cast<int>(threadIdx.x) & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+
+  // which rows: consecutive workgroups take the KV heads in turn (on 8 XCDs a head's keys then stay in few L2s);
+  // later row tiles, which see more keys where causal, come first
+  const uint32_t bid = blockIdx.x;
+  const uint32_t rest = div(bid, p.kv_heads);
+  const int head = static_cast<int>(bid - rest * p.kv_heads.d);
+  const uint32_t order = div(rest, p.splits);
+  const int split = static_cast<int>(rest - order * p.splits.d);
+  const int32_t idx = p.tiles - 1 - static_cast<int32_t>(order);
+  const int b = find_sequence<C::BM>(p, lane, idx);
+  const int32_t T = static_cast<int32_t>(p.T);
+  int32_t q0 = p.q_start[b], q1 = p.q_start[b + 1];
+  q0 = q0 < 0 ? 0 : q0 > T ? T : q0;
+  q1 = q1 < q0 ? q0 : q1 > T ? T : q1;
+  const int32_t G = static_cast<int32_t>(p.group.d), n = q1 - q0, R = n * G;
+  const int32_t row0 = (idx - static_cast<int32_t>(static_cast<int64_t>(q0) * G / C::BM) - b) * C::BM;
+  if (row0 < 0 || row0 >= R) return;
+  int32_t m = p.kv_len[b];
+  {
+    const int64_t most = p.ld_table << p.page_shift;
+    m = m < 0 ? 0 : m > most ? static_cast<int32_t>(most) : m;
+  }
+
+  // keys that the rows first .. last see
+  const int32_t ahead = m - n;  // position of the first new token
+  const auto range = [&](int32_t first, int32_t last) {
+    Range x;
+    x.lo = 0;
+    x.hi = m;
+    if (p.causal) {
+      const int32_t end = ahead + static_cast<int32_t>(div(last, p.group)) + 1;
+      x.hi = end < m ? end : m;
+      const int32_t from = ahead + static_cast<int32_t>(div(first, p.group)) + 1;
+      if (p.window && from > p.window) x.lo = from - p.window;
+    }
+    if (x.hi < 0) x.hi = 0;
+    if (x.lo > x.hi) x.lo = x.hi;
+    return x;
+  };
+  const int32_t row_end = row0 + C::BM < R ? row0 + C::BM : R;
+  const Range all = range(row0, row_end - 1);
+  // key tiles of the whole workgroup and of this split
+  const int32_t tile0 = all.lo / C::KT, tiles = all.hi > all.lo ? (all.hi + C::KT - 1) / C::KT - tile0 : 0;
+  int32_t per = (tiles + static_cast<int32_t>(p.splits.d) - 1) / static_cast<int32_t>(p.splits.d);
+  if (per < p.min_tiles) per = p.min_tiles;
+  const int32_t first = split * per, count = tiles - first < per ? tiles - first : per;
+  const int32_t j_begin = (tile0 + first) * C::KT;
+
+  // rows of this wavefront
+  const int32_t w0 = row0 + (C::SHARED ? wave * 16 * C::CB : 0);
+  const int32_t w1 = w0 + 16 * C::CB < R ? w0 + 16 * C::CB : R;
+  const bool busy = w0 < R;
+  Rows<C> w;
+  int32_t row[C::CB];
+  int64_t at_t[C::CB];  // token
+  int32_t at_h[C::CB];  // query head
+#pragma unroll
+  for (int cb = 0; cb < C::CB; ++cb) {
+    row[cb] = w0 + 16 * cb + (lane & 15);
+    const bool live = row[cb] < R;
+    const int32_t r = live ? row[cb] : R - 1;
+    const int32_t tok = static_cast<int32_t>(div(r, p.group));
+    at_t[cb] = q0 + tok;
+    at_h[cb] = head * G + r - tok * G;
+    const Range x = range(r, r);
+    w.lo[cb] = x.lo;
+    w.hi[cb] = x.hi;
+    w.m[cb] = neg_inf();
+    w.l[cb] = 0.0f;
+    const uint16_t* src = p.q + at_t[cb] * p.ldq + static_cast<int64_t>(at_h[cb]) * p.D;
+#pragma unroll
+    for (int step = 0; step < NS; ++step) {
+      const int d = 32 * step + 8 * (lane >> 4);
+      u32x4 u = {0u, 0u, 0u, 0u};
+      if (d < p.D) u = *reinterpret_cast<const u32x4*>(src + d);
+      w.q[step][cb] = __builtin_bit_cast(bf16x8, u);
+    }
+#pragma unroll
+    for (int db = 0; db < ND; ++db) w.o[db][cb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  // every row of the wavefront (workgroup) sees the keys full.lo .. full.hi - 1 (inner); some row those of any
+  const int32_t wf = busy ? w0 : R - 1, wl = busy ? w1 - 1 : R - 1;
+  const Range full{range(wl, wl).lo, range(wf, wf).hi}, any = range(wf, wl);
+  const Range inner{range(row_end - 1, row_end - 1).lo, range(row0, row0).hi};
+
+  const float k_scale = p.k.scale ? p.k.scale[head] : 1.0f, v_scale = p.v.scale ? p.v.scale[head] : 1.0f;
+  const float c = p.c * k_scale;
+  const auto in_part = [&](int32_t j0) { return j0 < inner.lo || j0 + C::KT > inner.hi; };
+  const auto step = [&](const Tiles<C>& t, int at, int32_t j0) {
+    if (!busy || j0 >= any.hi || j0 + C::KT <= any.lo) return;
+    tile_step(t, w, at, j0, c, j0 < full.lo || j0 + C::KT > full.hi);
+  };
+
+  if (threadIdx.x == 0) any_infinite = 0;
+  __syncthreads();
+  if (count > 0) {
+    Tiles<C> t(p, lds + (C::SHARED ? 0 : wave * 4 * C::TILE), lane, wave);
+    t.open(b, head, m, j_begin);
+    if constexpr (C::SHARED) {
+      t.request(j_begin, 0);
+      for (int32_t i = 0; i < count; ++i) {
+        const int32_t j0 = j_begin + i * C::KT;
+        wait_loads<0>();   // this wavefront's rows of tile i are there,
+        if (in_part(j0) && t.make_finite(i & 1)) any_infinite = 1;
+        group_barrier();   // every wavefront's are, and all have read tile i - 1
+        if (i + 1 < count) t.request(j0 + C::KT, (i + 1) & 1);
+        step(t, i & 1, j0);
+      }
+    } else {
+      if (wave < count) t.request(j_begin + wave * C::KT, 0);
+      int at = 0;
+      for (int32_t i = wave; i < count; i += C::WAVES, at ^= 1) {
+        const int32_t j0 = j_begin + i * C::KT;
+        if (i + C::WAVES < count) {
+          t.request(j0 + C::WAVES * C::KT, at ^ 1);
+          wait_loads<C::LOADS>();
+        } else {
+          wait_loads<0>();
+        }
+        if (in_part(j0) && t.make_finite(at)) any_infinite = 1;
+        step(t, at, j0);
+        asm volatile("" ::: "memory");  // the next request writes where this tile was read
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    __syncthreads();
+    if (any_infinite) {
+      for (int32_t i = C::SHARED ? 0 : wave; i < count; i += C::SHARED ? 1 : C::WAVES)
+        if (in_part(j_begin + i * C::KT)) add_infinities(t, w, j_begin + i * C::KT);
+    }
+  }
+
+  // a row's sum over the lanes that share it
+#pragma unroll
+  for (int cb = 0; cb < C::CB; ++cb) {
+    w.l[cb] += __shfl_xor(w.l[cb], 16);
+    w.l[cb] += __shfl_xor(w.l[cb], 32);
+  }
+  const bool whole = p.splits.d == 1;
+  const auto put = [&](int64_t tok, int32_t h, int d, f32x4 o, float bound, float sum, bool first_lane) {
+    // bound in log2 units; o, sum relative to it
+    const int64_t r = tok * p.n_q + h;
+    if (whole) {
+      const float f = sum == 0.0f ? 0.0f : v_scale / sum;
+      if (d < p.D) {
+        const u32x2 u = {pack_bf16x2(o[0] * f, o[1] * f), pack_bf16x2(o[2] * f, o[3] * f)};
+        *reinterpret_cast<u32x2*>(p.out + tok * p.ldo + static_cast<int64_t>(h) * p.D + d) = u;
+      }
+      if (first_lane && p.lse) p.lse[r] = sum == 0.0f ? neg_inf() : (bound + __builtin_amdgcn_logf(sum)) * kLn2;
+    } else {
+      const int64_t at = split * p.T * p.n_q + r;
+      if (d < p.D && sum != 0.0f) {
+        const f32x4 x = {o[0] * v_scale, o[1] * v_scale, o[2] * v_scale, o[3] * v_scale};
+        *reinterpret_cast<f32x4*>(p.part_o + at * p.D + d) = x;
+      }
+      if (first_lane) p.part_ml[at] = f32x2{bound, sum};
+    }
+  };
+  if constexpr (C::SHARED) {
+#pragma unroll
+    for (int cb = 0; cb < C::CB; ++cb)
+      if (row[cb] < R)
+#pragma unroll
+        for (int db = 0; db < ND; ++db)
+          put(at_t[cb], at_h[cb], 16 * db + 4 * (lane >> 4), w.o[db][cb], w.m[cb] * c, w.l[cb], db == 0 && lane < 16);
+  } else {
+    // join the wavefronts, in ascending order: rows of (DT + 4) floats, then bounds, then sums
+    float* rows = reinterpret_cast<float*>(lds);
+    float* bounds = rows + C::WAVES * 16 * C::CB * C::JOIN_ROW;
+    float* sums = bounds + C::WAVES * 16 * C::CB;
+    __syncthreads();
+#pragma unroll
+    for (int cb = 0; cb < C::CB; ++cb) {
+      const int i = (wave * C::CB + cb) * 16 + (lane & 15);
+      if (lane < 16) {
+        bounds[i] = w.m[cb] * c;
+        sums[i] = w.l[cb];
+      }
+#pragma unroll
+      for (int db = 0; db < ND; ++db)
+        *reinterpret_cast<f32x4*>(rows + i * C::JOIN_ROW + 16 * db + 4 * (lane >> 4)) = w.o[db][cb];
+    }
+    __syncthreads();
+    constexpr int kVecs = C::DT / 4, kAll = 16 * C::CB * kVecs, kThreads = 64 * C::WAVES;
+    for (int u = static_cast<int>(threadIdx.x); u < kAll; u += kThreads) {
+      const int i = u / kVecs, d = (u % kVecs) * 4;
+      const int32_t r = row0 + i;
+      if (r >= R) break;
+      float top = neg_inf();
+#pragma unroll
+      for (int x = 0; x < C::WAVES; ++x) top = fmaxf(top, bounds[x * 16 * C::CB + i]);
+      float sum = 0.0f;
+      f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int x = 0; x < C::WAVES; ++x) {
+        const float f = __builtin_amdgcn_exp2f(bounds[x * 16 * C::CB + i] - (top == neg_inf() ? 0.0f : top));
+        sum += f * sums[x * 16 * C::CB + i];
+        const f32x4 v = *reinterpret_cast<const f32x4*>(rows + (x * 16 * C::CB + i) * C::JOIN_ROW + d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += f * v[e];
+      }
+      const int32_t tok = static_cast<int32_t>(div(r, p.group));
+      put(q0 + tok, head * G + r - tok * G, d, o, top, sum, d == 0);
+    }
+  }
+}
+
+template <class C>
+Variant variant(const char* name) {
+  return Variant{reinterpret_cast<const void*>(&qkn_attn_kernel<C>), C::BM, C::KT * C::STAGES, 64 * C::WAVES, C::LDS, name};
+}
+
+// A kernel for sequences of up to `rows` rows, and one for more. dt: 64, 128 or 256.
+__attribute__((visibility("hidden"))) Variant few_rows(int dt, bool fp8, int rows);
+__attribute__((visibility("hidden"))) Variant many_rows(int dt, bool fp8);
+
+}  // namespace attn
+
+#endif  // QKN_ATTN_KERNELS_H

@@ -1,0 +1,265 @@
+"""Attention over the paged cache, against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_09160_amd as qkn
+from oracle import block as O
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _host(t):
+    return t.detach().double().cpu().numpy()
+
+
+class Batch:
+    """A batch of sequences with shuffled pages; what no token sees is filled with NaN."""
+
+    def __init__(self, seed, lens, hq, hk, D, page=16, fp8=False, spread=1.0, order="heads first", pad=0):
+        g = torch.Generator().manual_seed(seed)
+        self.lens, self.hq, self.hk, self.D, self.page, self.fp8 = lens, hq, hk, D, page, fp8
+        self.T = sum(n for n, _ in lens)
+        counts = [(m + page - 1) // page for _, m in lens]
+        pages = sum(counts) + 2
+        perm = torch.randperm(pages, generator=g)
+        width = max(counts + [1])
+        self.table = torch.full((len(lens), width), pages + 7, dtype=torch.int32)  # unused entries: no such page
+        at = 0
+        for b, c in enumerate(counts):
+            self.table[b, :c] = perm[at:at + c].int()
+            at += c
+        used = torch.zeros(pages, page, dtype=torch.bool)
+        for b, (n, m) in enumerate(lens):
+            for j in range(m):
+                used[self.table[b, j // page], j % page] = True
+        pools = []
+        for _ in range(2):
+            x = torch.randn(pages, hk, page, D, generator=g) * spread
+            x = x.to(torch.float8_e4m3fn).float() if fp8 else x.to(torch.bfloat16).float()
+            x = torch.where(used[:, None, :, None], x, torch.nan)
+            pools.append(x)
+        self.k, self.v = pools
+        self.scales = [torch.rand(hk, generator=g) + 0.5 if fp8 else None for _ in range(2)]
+        self.q = (torch.randn(self.T, hq * D, generator=g) * spread).to(torch.bfloat16)
+        self.order, self.pad = order, pad
+        self.q_start = torch.tensor(np.concatenate([[0], np.cumsum([n for n, _ in lens])]), dtype=torch.int32)
+        self.kv_len = torch.tensor([m for _, m in lens], dtype=torch.int32)
+
+    def _pool(self, x):
+        x = x.to(torch.float8_e4m3fn if self.fp8 else torch.bfloat16).to(DEV)
+        if self.order == "rows first":
+            raw = x.view(torch.uint8 if self.fp8 else torch.int16)
+            x = raw.transpose(1, 2).contiguous().transpose(1, 2).view(x.dtype)
+        return x
+
+    def run(self, lse=True, **kw):
+        q = torch.zeros(self.T, self.hq * self.D + self.pad, dtype=torch.bfloat16, device=DEV)[:, :self.hq * self.D]
+        q.copy_(self.q)
+        s = [z.to(DEV) if z is not None else None for z in self.scales]
+        lse = torch.full((self.T, self.hq), 7.0, device=DEV) if lse else None
+        kw = {"max_q": max([n for n, _ in self.lens] + [0]), "max_kv": max([m for _, m in self.lens] + [0]), **kw}
+        out = qkn.qkn_attn(q, qkn.KVCache(self._pool(self.k), self._pool(self.v), *s), self.table.to(DEV),
+                           self.q_start.to(DEV), self.kv_len.to(DEV), lse=lse, **kw)
+        torch.cuda.synchronize()
+        return out, lse
+
+    def sequence(self, b, h):
+        """q, k, v of one sequence and query head, in 64 bits."""
+        n, m = self.lens[b]
+        pages = self.table[b, :(m + self.page - 1) // self.page].long()
+        g = h // (self.hq // self.hk)
+        k, v = (z[pages, g].reshape(-1, self.D)[:m].double().numpy() * (float(s[g]) if s is not None else 1.0)
+                for z, s in ((self.k, self.scales[0]), (self.v, self.scales[1])))
+        t = int(self.q_start[b])
+        return self.q[t:t + n, h * self.D:(h + 1) * self.D].double().numpy(), k, v
+
+    def check(self, out, lse, scale=None, causal=True, window=0):
+        out, lse = _host(out), _host(lse)
+        scale = self.D ** -0.5 if scale is None else scale
+        for b, (n, m) in enumerate(self.lens):
+            t = int(self.q_start[b])
+            for h in range(self.hq):
+                q, k, v = self.sequence(b, h)
+                ref, ref_lse = O.attention(q, k, v, scale, causal, window)
+                size, _ = O.attention(q, k, np.abs(v), scale, causal, window)
+                # fp32 scores: sums of 32 products at a time (16 roundings at most) and the exponent's argument, relative to
+                # the largest terms
+                reach = scale * np.abs(q).max(initial=0) * np.abs(k).max(initial=0) * self.D
+                e = 2.0 ** -20 * (reach + np.log2(m + 2) + 4)
+                # weights rounded to bf16 (2^-8 at most, half of it their share of the sum apart), then the result
+                got = out[t:t + n, h * self.D:(h + 1) * self.D]
+                O.check_rounded(got, ref, (2.0 ** -8 + 2 * e) * size, "bf16", f"sequence {b} head {h}")
+                empty = np.isneginf(ref_lse)
+                assert np.array_equal(np.isneginf(lse[t:t + n, h]), empty)
+                bad = np.isnan(ref_lse)
+                assert np.array_equal(np.isnan(lse[t:t + n, h]), bad)
+                ok = ~empty & ~bad
+                assert np.all(np.abs(lse[t:t + n, h][ok] - ref_lse[ok]) <= e + 2.0 ** -22 * np.abs(ref_lse[ok]))
+
+
+LENGTHS = {
+    "one token, one key": [(1, 1)],
+    "single tokens": [(1, 1), (1, 15), (1, 16), (1, 17), (1, 31), (1, 32), (1, 33), (1, 64), (1, 130), (1, 700)],
+    "prompt": [(67, 67)],
+    "chunk": [(33, 300)],
+    "mixed": [(1, 200), (0, 0), (70, 70), (1, 1), (0, 50), (19, 128), (5, 6)],
+    "long chunk": [(200, 523)],
+}
+
+
+@pytest.mark.parametrize("lens", list(LENGTHS))
+@pytest.mark.parametrize("hq,hk,D,page,fp8", [(1, 1, 64, 16, False), (4, 1, 128, 16, False), (5, 1, 128, 32, True),
+                                              (6, 2, 64, 64, True), (8, 2, 256, 16, False), (4, 4, 256, 128, True),
+                                              (8, 1, 96, 16, False), (2, 2, 8, 16, False), (24, 1, 32, 16, True)])
+def test_against_the_definition(lens, hq, hk, D, page, fp8):
+    batch = Batch(len(lens) * 100 + D, LENGTHS[lens], hq, hk, D, page, fp8)
+    batch.check(*batch.run())
+
+
+@pytest.mark.parametrize("window", [1, 2, 16, 33, 100, 10000])
+@pytest.mark.parametrize("hq,hk", [(2, 2), (16, 1), (40, 1)])
+def test_windows(window, hq, hk):
+    batch = Batch(window, [(1, 300), (40, 40), (3, 90), (65, 210)], hq, hk, 64)
+    batch.check(*batch.run(window=window), window=window)
+
+
+@pytest.mark.parametrize("hq,hk", [(2, 2), (16, 1), (40, 1)])
+def test_not_causal(hq, hk):
+    batch = Batch(5, [(1, 300), (40, 40), (3, 90), (20, 7)], hq, hk, 64)
+    batch.check(*batch.run(causal=False), causal=False)
+
+
+@pytest.mark.parametrize("hq,hk", [(1, 1), (16, 1), (40, 1)])
+def test_rows_that_see_nothing(hq, hk):
+    """More new tokens than the cache holds: the first ones are before its first token."""
+    batch = Batch(8, [(20, 7), (9, 0), (3, 3), (80, 1)], hq, hk, 128)
+    out, lse = batch.run()
+    batch.check(out, lse)
+    assert out[:13].abs().max() == 0 and lse[:13].isneginf().all() and out[20:29].abs().max() == 0
+
+
+@pytest.mark.parametrize("few", [True, False])
+@pytest.mark.parametrize("max_kv", [1, 500, 4000])
+def test_hints_do_not_change_what_is_computed(few, max_kv):
+    """max_q and max_kv choose the kernel and the splits; lengths beyond them stay right."""
+    batch = Batch(11, [(1, 900), (70, 300), (2, 33)], 8, 2, 128)
+    batch.check(*batch.run(max_q=1 if few else 4096, max_kv=max_kv))
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("order,pad", [("rows first", 8), ("heads first", 16)])
+def test_strides(order, pad, fp8):
+    batch = Batch(12, [(1, 70), (50, 99)], 4, 2, 64, 32, fp8, order=order, pad=pad)
+    batch.check(*batch.run())
+
+
+@pytest.mark.parametrize("hq", [4, 80])
+@pytest.mark.parametrize("spread", [0.05, 6.0, 30.0])
+def test_flat_and_peaked_weights(hq, spread):
+    batch = Batch(13, [(1, 1000), (30, 400)], hq, 1, 128, spread=spread)
+    batch.check(*batch.run(max_kv=1000), scale=None)
+
+
+def test_rising_scores_move_the_bound():
+    """Each key's score is far above all before it: every tile rescales what came before."""
+    batch = Batch(14, [(1, 600), (3, 600), (40, 600)], 4, 1, 64)
+    steps = torch.arange(600).float() * 0.25
+    for b in range(3):
+        pages = batch.table[b, :38].long()
+        for j in range(600):
+            batch.k[pages[j // 16], 0, j % 16] = (torch.ones(64) * steps[j]).to(torch.bfloat16).float()
+    batch.q = torch.full_like(batch.q, 1.0)
+    batch.check(*batch.run())
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("hq,window", [(4, 0), (40, 0), (2, 20), (40, 20), (130, 20)])
+@pytest.mark.parametrize("value", ["nan", "inf"])
+def test_unseen_infinities_and_nan_reach_no_row(fp8, hq, window, value):
+    """A key's NaN or infinity, in K or in V, is in the result of the tokens that see the key and of no other."""
+    if fp8 and value == "inf":
+        pytest.skip("e4m3fn has no infinity")
+    n, m = 37, 150
+    batch = Batch(15, [(n, m), (1, 64)], hq, 1, 64, 16, fp8)
+    clean_out, clean_lse = batch.run(window=window)
+    for pool, element in (("v", 5), ("v", 63), ("k", 9)):
+        for j in (m - n - 3, m - n + 4, m - 20, m - 1):
+            bad = Batch(15, [(n, m), (1, 64)], hq, 1, 64, 16, fp8)
+            getattr(bad, pool)[int(bad.table[0, j // 16]), 0, j % 16, element] = float(value)
+            out, _ = bad.run(window=window)
+            at = torch.arange(m - n, m)
+            sees = (at >= j) & ((at < j + window) if window else torch.tensor(True))
+            same = out[:n].view(n, hq, 64) == clean_out[:n].view(n, hq, 64)
+            assert same[~sees].all(), (pool, element, j)
+            assert torch.equal(out[n:], clean_out[n:])
+            if pool == "v":
+                hit = out[:n].view(n, hq, 64)[..., element]
+                assert (hit[sees].isnan() if value == "nan" else hit[sees] == float("inf")).all()
+                same[..., element] = True
+                assert same.all()
+
+
+def test_table_entries_and_lengths_outside_their_ranges_stay_inside_the_buffers():
+    batch = Batch(16, [(1, 40), (20, 60)], 4, 1, 64)
+    batch.table[0, 1], batch.table[1, 2] = -5, 1 << 30
+    batch.kv_len[1] = 1 << 30
+    batch.q_start[0] = -3
+    out, _ = batch.run(max_kv=64)
+    assert out.shape == (21, 256)
+    zero = Batch(16, [(1, 40)], 4, 1, 64)
+    zero.table[0, :] = -1  # no page: keys and values of zero
+    out, lse = zero.run()
+    assert out.abs().max() == 0 and torch.allclose(lse, torch.full_like(lse, float(np.log(40.0))), atol=1e-5)
+
+
+def test_repeats_graphs_and_streams_agree():
+    batch = Batch(17, [(1, 1500), (1, 20), (1, 800)], 8, 2, 128)
+    want, want_lse = batch.run()
+    for _ in range(3):
+        out, lse = batch.run()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    kv_len = batch.kv_len.to(DEV)
+    lse = torch.empty(3, 8, device=DEV)
+    call = qkn.PreparedAttn(batch.q.to(DEV), qkn.KVCache(batch._pool(batch.k), batch._pool(batch.v)),
+                            batch.table.to(DEV), batch.q_start.to(DEV), kv_len, max_q=1, max_kv=1500, lse=lse)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.synchronize()
+    assert torch.equal(call.out, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(3):  # a replay reads the lengths that the device holds then
+        for lens in ((1500, 20, 800), (1499, 7, 1)):
+            kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+            call.out.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            batch.lens = [(1, m) for m in lens]
+            batch.check(call.out, lse)
+
+
+def test_no_tokens():
+    batch = Batch(18, [(0, 0), (0, 30)], 2, 1, 64)
+    out, _ = batch.run()
+    assert out.shape == (0, 128)
+
+
+@pytest.mark.parametrize("hq,hk,D,fp8,n,m", [(16, 4, 128, False, 777, 3000), (5, 1, 128, True, 1, 20000),
+                                             (8, 2, 64, False, 1024, 1024), (4, 1, 256, True, 300, 2100)])
+def test_long(hq, hk, D, fp8, n, m):
+    batch = Batch(19, [(n, m)], hq, hk, D, 64, fp8)
+    out, lse = batch.run()
+    rows = sorted({0, min(1, n - 1), n // 3, n // 2, n - 1})
+    for h in (0, hq - 1):
+        q, k, v = batch.sequence(0, h)
+        for i in rows:
+            ref, ref_lse = O.attention(q[i:i + 1], k[:m - n + i + 1], v[:m - n + i + 1], D ** -0.5)
+            size, _ = O.attention(q[i:i + 1], k[:m - n + i + 1], np.abs(v[:m - n + i + 1]), D ** -0.5)
+            e = 2.0 ** -20 * (D ** -0.5 * np.abs(q[i]).max() * np.abs(k).max() * D + 20)
+            O.check_rounded(_host(out)[i, h * D:(h + 1) * D], ref[0], (2.0 ** -8 + 2 * e) * size[0], "bf16", f"{i} {h}")
+            assert abs(_host(lse)[i, h] - ref_lse[0]) <= e + 2.0 ** -22 * abs(ref_lse[0])
