@@ -1,4 +1,4 @@
-"""ctypes binding of the attention block's entry points (include/qkn_rope.h, qkn_attn.h, qkn_cache.h): argument marshalling
+"""ctypes binding of the attention block's entry points (include/qkn_rope.h, qkn_attn.h, qkn_adapters.h, qkn_cache.h): argument marshalling
 only, as in ``_lib``.
 
 Row tensors are 2-D with a contiguous last dimension and any row stride; heads follow each other in a row, as
@@ -42,6 +42,12 @@ class QknAttnArgs(ctypes.Structure):
                 ("scale", ctypes.c_float)]
 
 
+class QknAdapterSeg(ctypes.Structure):
+    _fields_ = [("a", _vp), ("a_adapter", _c_i64), ("lda", _c_i64), ("b", _vp), ("b_adapter", _c_i64),
+                ("ldb", _c_i64), ("base", _vp), ("ldbase", _c_i64), ("y", _vp), ("ldy", _c_i64), ("partials", _vp),
+                ("d_local", _c_i64)]
+
+
 def load() -> ctypes.CDLL:
     """The library with these entry points' signatures declared."""
     lib = _load()
@@ -53,6 +59,10 @@ def load() -> ctypes.CDLL:
         lib.qkn_attn_workspace_bytes.argtypes = [ctypes.POINTER(QknAttnArgs), ctypes.POINTER(QknCache)]
         lib.qkn_attn_workspace_bytes.restype = _c_i64
         lib.qkn_attn.argtypes = [ctypes.POINTER(QknAttnArgs), ctypes.POINTER(QknCache), _vp, _c_i64, _vp]
+        lib.qkn_adapters_workspace_bytes.argtypes = [_c_i64, _c_i64, _int, _int]
+        lib.qkn_adapters_workspace_bytes.restype = _c_i64
+        lib.qkn_adapters_add.argtypes = [_vp, _c_i64, _c_i64, _c_i64, ctypes.POINTER(QknAdapterSeg), _int, _int, _c_i64,
+                                         _vp, _vp, _vp, _c_i64, _vp]
     return lib
 
 
@@ -262,3 +272,71 @@ def qkn_attn(q, cache, block_table, q_start, kv_len, max_q=None, max_kv=None, sc
     """PreparedAttn made and called once."""
     return PreparedAttn(q, cache, block_table, q_start, kv_len, max_q, max_kv, scale, causal, window, out, lse,
                         workspace)(stream)
+
+
+@dataclass
+class AdapterSeg:
+    """One output (Q, K or V) of the adapters: a bf16 [adapters, rank, hidden], b bf16 [adapters, d_local, rank] (any
+    strides with a contiguous last dimension), base the projection's rows (None: y, in place)."""
+
+    a: torch.Tensor
+    b: torch.Tensor
+    y: Optional[torch.Tensor] = None         # bf16 [T, d_local]; allocated if None and base is given
+    partials: Optional[torch.Tensor] = None  # fp32 [T]; not taken if None
+    base: Optional[torch.Tensor] = None      # bf16 [T, d_local]
+
+
+def _matrices(t: torch.Tensor, what: str):
+    """(pointer, stride of an adapter, stride of a row) of a [adapters, rows, columns] tensor."""
+    if t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{what}: expected a bf16 GPU tensor [adapters, rows, columns], last dimension contiguous")
+    return t.data_ptr(), t.stride(0), t.stride(1) if t.shape[1] > 1 else max(t.stride(1), t.shape[2])
+
+
+class PreparedAdapters:
+    """qkn_adapters_add with its arguments and workspace prepared once: y = base + scale_i B_i A_i x for the tokens
+    of each request's adapter i = ids[t] (int32 [T]; outside the adapters: none), and the Phase A statistic of the
+    stored rows. x is the projection's input (bf16 [T, hidden]), scale fp32 [adapters] or None."""
+
+    def __init__(self, x: torch.Tensor, segs, ids: torch.Tensor, scale: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None):
+        px, ldx, T, hidden = _rows(x, "x")
+        segs = list(segs)
+        if not 1 <= len(segs) <= 3:
+            raise ValueError("1 to 3 segments are expected")
+        count, rank = segs[0].a.shape[:2] if segs[0].a.dim() == 3 else (0, 0)
+        arr = (QknAdapterSeg * len(segs))()
+        for i, s in enumerate(segs):
+            a, b = _matrices(s.a, f"seg{i}.a"), _matrices(s.b, f"seg{i}.b")
+            d = s.b.shape[1]
+            if tuple(s.a.shape) != (count, rank, hidden) or tuple(s.b.shape) != (count, d, rank):
+                raise ValueError(f"seg{i}: expected a [{count}, {rank}, {hidden}] and b [{count}, d, {rank}], got "
+                                 f"{tuple(s.a.shape)}, {tuple(s.b.shape)}")
+            if s.y is None:
+                if s.base is None:
+                    raise ValueError(f"seg{i}: base, y or both must be given")
+                s.y = torch.empty((T, d), dtype=s.base.dtype, device=s.base.device)
+            py, ldy, Ty, wy = _rows(s.y, f"seg{i}.y")
+            pb, ldb, Tb, wb = (py, ldy, Ty, wy) if s.base is None else _rows(s.base, f"seg{i}.base")
+            if (Ty, wy) != (T, d) or (Tb, wb) != (T, d):
+                raise ValueError(f"seg{i}: y and base must be [{T}, {d}]")
+            arr[i] = QknAdapterSeg(*a, *b, pb, ldb, py, ldy, _f32(s.partials, f"seg{i}.partials", T), d)
+        lib = load()
+        need = lib.qkn_adapters_workspace_bytes(T, hidden, rank, len(segs))
+        if need < 0:
+            _check(int(need), "qkn_adapters_workspace_bytes")
+        self.workspace = _workspace(workspace, need, x.device)
+        self.segs = segs
+        self._keep = (x, ids, scale)
+        self._args = (px, ldx, T, hidden, arr, len(segs), rank, count, _index(ids, "ids", torch.int32, T),
+                      _f32(scale, "scale", count), self.workspace.data_ptr(), self.workspace.numel())
+        self._fn = lib.qkn_adapters_add
+
+    def __call__(self, stream=None):
+        _check(self._fn(*self._args, _stream(stream)), "qkn_adapters_add")
+        return [(s.y, s.partials) for s in self.segs]
+
+
+def qkn_adapters_add(x, segs, ids, scale=None, workspace=None, stream=None):
+    """PreparedAdapters made and called once; returns the segments' (y, partials)."""
+    return PreparedAdapters(x, segs, ids, scale, workspace)(stream)
