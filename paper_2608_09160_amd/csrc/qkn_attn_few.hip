@@ -3,9 +3,12 @@
 
 namespace attn {
 
-// 32 keys a tile; as many wavefronts as the LDS has buffers for.
+// 32 keys a tile; as many workgroups on a CU as registers and LDS have room for.
+constexpr int occupancy(int dt, bool fp8, int cb) {
+  return cb == 1 ? (dt == 64 || (dt == 128 && fp8) ? 4 : dt == 128 ? 2 : 1) : dt == 64 || (dt == 128 && cb == 2) ? 2 : 1;
+}
 template <int DT, bool FP8, int CB>
-using Few = Cfg<DT, FP8, CB, (DT == 256 && !FP8 ? 2 : 4), false, 32, 1>;
+using Few = Cfg<DT, FP8, CB, 4, false, 32, occupancy(DT, FP8, CB)>;
 
 template <int DT, bool FP8>
 static Variant pick(int rows, const char* n1, const char* n2, const char* n4) {

@@ -15,18 +15,20 @@
 // (`kSlack`): most tiles then need no maximum across lanes and no rescaling. Weights are at most 2^8, which changes
 // nothing in their relative rounding. The sum l is of the unrounded fp32 weights.
 //
-// Tiles. KT keys at a time, K and V rows straight from the cache's pages into LDS (buffer_load ... lds, 16 bytes a
-// lane), two buffers, the next tile in flight while one is computed. A wavefront fetches 16 rows at a time: they lie
-// in one page, whose descriptor ends at the sequence's last token (or has no bytes for a bad page number), so rows
-// past it read zeros. 16-byte chunks of a row are stored at chunk ^ f(row), f such that the rows of one LDS read
-// fall on different banks.
+// Tiles. KT keys at a time, rows straight from the cache's pages into LDS (buffer_load ... lds, 16 bytes a lane), two
+// buffers, the next tile in flight while one is computed. A wavefront fetches 16 rows at a time: they lie in one page,
+// whose descriptor ends at the sequence's last token (or has no bytes for a bad page number), so rows past it read
+// zeros. 16-byte chunks of a row are stored at chunk ^ f(row), f such that the rows of one LDS read fall on different
+// banks.
 //
 // Two ways to share the work of a workgroup:
 //   SHARED  every wavefront has its own 16 CB rows, all take the same key tiles (many rows: products bound it);
 //   !SHARED every wavefront takes its own key tiles for the same 16 CB rows, with no barrier in the loop, and the
-//           wavefronts' results are joined at the end (few rows: bytes bound it).
-// Over workgroups the keys are split further where rows alone do not fill the chip; qkn_attn_join adds the parts in
-// ascending order.
+//           wavefronts' results are joined at the end (few rows: bytes bound it). No other wavefront wants its K rows,
+//           and a row is an operand as it is: they go to registers, LDS has V only, and with half the LDS a CU holds
+//           twice the wavefronts, so twice the bytes are on their way.
+// Over workgroups the keys are split further where rows alone do not fill the chip (`schedule`); qkn_attn_join adds the
+// parts in ascending order.
 #ifndef QKN_ATTN_KERNELS_H
 #define QKN_ATTN_KERNELS_H
 
@@ -58,22 +60,24 @@ struct Params {
   const int32_t* table;
   int64_t ldq, ldo, ld_table, T;
   Pool k, v;
-  int64_t num_pages;
+  uint32_t num_pages;
   int32_t page_shift;
-  int32_t batch, n_q, n_kv, D, tiles;  // tiles: row tiles of the grid
+  int32_t batch, n_q, n_kv, D;
+  int32_t items;                       // workgroups of a KV head
   int32_t causal, window;
   float c;                             // scale * log2(e)
-  FastDiv group, kv_heads, splits;
-  // split keys: split s of row (t, h) at index (s T + t) n_q + h
-  float* part_o;                       // [splits, T * n_q, D]
-  f32x2* part_ml;                      // [splits, T * n_q]: bound (log2 units) and sum; sum 0: nothing
-  int32_t min_tiles;                   // key tiles of a split, at least
+  FastDiv group, kv_heads;
+  // split keys (NULL: not split): what each workgroup has of its row tile, and which workgroups have a row's parts
+  float* part_o;                       // [workgroups, BM, D]
+  f32x2* part_ml;                      // [workgroups, BM]: bound (log2 units) and sum; sum 0: nothing
+  int32_t (*parts_of)[2];              // [T * n_q]: workgroup of the first part; parts * 256 + row of the tile
+  int32_t min_part;                    // key steps of a part, at least
 };
 
 // A kernel and what its launch has to know.
 struct Variant {
   const void* fn;
-  int rows, keys, threads, lds;  // rows of a workgroup; keys that its wavefronts take at a time, in all
+  int rows, step, threads, lds, slots;  // rows of a workgroup; keys that it takes at a time; workgroups of a CU
   const char* name;
 };
 
@@ -108,6 +112,10 @@ template <int DT_, bool FP8_, int CB_, int WAVES_, bool SHARED_, int KT_, int OC
 struct Cfg {
   static constexpr int DT = DT_, CB = CB_, WAVES = WAVES_, KT = KT_, OCC = OCC_;
   static constexpr bool FP8 = FP8_, SHARED = SHARED_;
+#ifndef QKN_AHEAD
+#define QKN_AHEAD 2
+#endif
+  static constexpr int AHEAD = QKN_AHEAD;
   static constexpr int ES = FP8 ? 1 : 2;
   static constexpr int RB = DT * ES;              // bytes of an LDS row
   static constexpr int CH = RB / 16;              // its 16-byte chunks
@@ -115,15 +123,21 @@ struct Cfg {
   static constexpr int PER256 = RB >= 256 ? 1 : 256 / RB;  // rows of one pass over the banks
   static constexpr int BM = 16 * CB * (SHARED ? WAVES : 1);  // rows of a workgroup
   static constexpr int TILE = KT * RB;            // bytes of a K (V) tile
+  static constexpr int BUF = (SHARED ? 2 : 1) * TILE;  // a buffer: K and V, or V
+  static constexpr int V_AT = SHARED ? TILE : 0;  // V in it
+  static constexpr int STEP = KT * (SHARED ? 1 : WAVES);  // keys that a workgroup takes at a time
+  static constexpr int KL = DT * ES / 64;         // 16-byte loads of 16 K rows into registers (!SHARED)
   static constexpr int BLOCKS = SHARED ? KT / 16 / WAVES : KT / 16;  // 16-row blocks that a wavefront loads
-  static constexpr int LOADS = 2 * BLOCKS * 16 / RPL;  // load instructions of a wavefront per tile
+  static constexpr int V_LOADS = BLOCKS * 16 / RPL;  // load instructions of a wavefront for a V tile
   static constexpr int STAGES = SHARED ? 1 : WAVES;    // key streams of a workgroup
   static constexpr int JOIN_ROW = DT + 4;         // floats of a row while wavefronts are joined
   static constexpr int JOIN = SHARED ? 0 : WAVES * 16 * CB * (JOIN_ROW + 2) * 4;
-  static constexpr int LDS = 4 * TILE * STAGES > JOIN ? 4 * TILE * STAGES : JOIN;
+  static constexpr int LDS = 2 * BUF * STAGES > JOIN ? 2 * BUF * STAGES : JOIN;
   static_assert(!SHARED || KT == 16 * WAVES, "a block of 16 rows for every wavefront");
+  static constexpr int SLOTS = OCC < 160 * 1024 / LDS ? OCC : 160 * 1024 / LDS;  // workgroups that a CU holds
+  static_assert(WAVES == 4, "a wavefront of a workgroup on each SIMD");
   static_assert(LDS <= 160 * 1024, "LDS");
-  static_assert(CH <= 64 && LOADS < 64, "loads");
+  static_assert(CH <= 64 && V_LOADS < 64, "loads");
   // Chunk c of row r is stored at c ^ swizzle(r). K: 16 lanes read the same chunk of 16 rows.
   __device__ static constexpr int swizzle_k(int r) { return (r / PER256) & ((CH < 16 ? CH : 16) - 1); }
   // V, bf16: 32 lanes read 2 chunks of 8 rows. FP8: one chunk of rows 0 to 7 and 16 to 23.
@@ -138,10 +152,30 @@ struct Range {
   int32_t lo, hi;
 };
 
+// The transposing LDS reads. `filling` is the buffer that loads in flight write, which the read does not touch: without
+// being told, the compiler waits for all of them before each of these reads (unlike before plain ones).
+__device__ __forceinline__ s16x4 read_tr16(unsigned char* src, const unsigned char* __restrict filling) {
+  if (filling == src) __builtin_unreachable();
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src));
+}
+__device__ __forceinline__ i32x2 read_tr8(unsigned char* src, const unsigned char* __restrict filling) {
+  if (filling == src) __builtin_unreachable();
+  return __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(src));
+}
+
+template <bool FP8>
+struct RawOf {
+  using T = u32x4;
+};
+template <>
+struct RawOf<true> {
+  using T = i32x2;
+};
+
 template <class C>
 struct Tiles {
   // One wavefront's view of the key tiles: which lane fetches and reads what.
-  unsigned char* buf;       // its stream's two buffers: K, V, K, V
+  unsigned char* buf;       // its stream's two buffers
   int lane, wave;
   const Params& p;
   int64_t head_k, head_v;   // bytes to the head
@@ -167,35 +201,59 @@ struct Tiles {
     cur = entry(page0 + lane);
     next = entry(page0 + 64 + lane);
   }
-  // Requests rows [j0, j0 + KT) (SHARED: this wavefront's 16 of them) into buffer `at`.
+  // The 16 rows from key j on: page, row in it, and how many of them the sequence has.
+  struct Where {
+    int64_t page, row0;
+    uint32_t rows;
+  };
+  __device__ __forceinline__ Where where(int32_t j) {
+    const int32_t pi = j >> p.page_shift;
+    while (pi - page0 >= 64) {  // pages are taken in ascending order
+      cur = next;
+      page0 += 64;
+      next = entry(page0 + 64 + lane);
+    }
+    const int32_t page = __builtin_amdgcn_readlane(cur, pi - page0);
+    const int32_t left = kv_len - j;
+    const int32_t rows = static_cast<uint32_t>(page) >= p.num_pages ? 0 : left < 0 ? 0 : left < 16 ? left : 16;
+    return Where{rows ? page : 0, j & ((1 << p.page_shift) - 1), static_cast<uint32_t>(rows)};
+  }
+  __device__ __forceinline__ Rsrc rows_of(const Pool& pool, int64_t head, const Where& w) const {
+    // scalars, as they are the same on all lanes: a descriptor in vector registers costs a loop around every load
+    const uint32_t bytes = __builtin_amdgcn_readfirstlane(w.rows ? w.rows * pool.token - (pool.token - p.D * C::ES) : 0);
+    return rsrc(pool.base + w.page * pool.page + head + w.row0 * pool.token, bytes);
+  }
+  // One load instruction's rows of a 16-row block into LDS.
+  __device__ __forceinline__ void load_rows(Rsrc r, uint32_t token, unsigned char* dst, int row, int chunk) {
+    load_to_lds(r, dst, chunk * 16 < p.D * C::ES ? row * token + chunk * 16 : 0x7fffffffu);
+  }
+  // Requests rows [j0, j0 + KT) (SHARED: this wavefront's 16 of them) into buffer `at`; !SHARED: V's only.
   __device__ __forceinline__ void request(int32_t j0, int at) {
-    unsigned char* kbuf = buf + at * 2 * C::TILE;
+    unsigned char* dst = buf + at * C::BUF;
 #pragma unroll
     for (int bl = 0; bl < C::BLOCKS; ++bl) {
       const int blk = C::SHARED ? wave : bl;
-      const int32_t j = j0 + 16 * blk;
-      const int32_t pi = j >> p.page_shift;
-      while (pi - page0 >= 64) {  // pages are taken in ascending order
-        cur = next;
-        page0 += 64;
-        next = entry(page0 + 64 + lane);
-      }
-      const int32_t page = __builtin_amdgcn_readlane(cur, pi - page0);
-      const int32_t row0 = j & ((1 << p.page_shift) - 1);
-      const int32_t left = kv_len - j;
-      const uint32_t rows = left < 0 || static_cast<uint32_t>(page) >= p.num_pages ? 0 : left < 16 ? left : 16;
-      const uint32_t k_bytes = rows ? (rows - 1) * p.k.token + p.D * C::ES : 0;
-      const uint32_t v_bytes = rows ? (rows - 1) * p.v.token + p.D * C::ES : 0;
-      const int64_t pg = rows ? page : 0;
-      const Rsrc rk = rsrc(p.k.base + pg * p.k.page + head_k + static_cast<int64_t>(row0) * p.k.token, k_bytes);
-      const Rsrc rv = rsrc(p.v.base + pg * p.v.page + head_v + static_cast<int64_t>(row0) * p.v.token, v_bytes);
+      const Where w = where(j0 + 16 * blk);
+      const Rsrc rk = rows_of(p.k, head_k, w), rv = rows_of(p.v, head_v, w);
 #pragma unroll
       for (int i = 0; i < 16 / C::RPL; ++i) {
-        const int r = i * C::RPL + lane / C::CH;
-        const int ck = (lane % C::CH) ^ C::swizzle_k(r), cv = (lane % C::CH) ^ C::swizzle_v(r + 16 * blk);
-        unsigned char* dst = kbuf + (16 * blk + i * C::RPL) * C::RB;
-        load_to_lds(rk, dst, ck * 16 < p.D * C::ES ? r * p.k.token + ck * 16 : 0x7fffffffu);
-        load_to_lds(rv, dst + C::TILE, cv * 16 < p.D * C::ES ? r * p.v.token + cv * 16 : 0x7fffffffu);
+        const int r = i * C::RPL + lane / C::CH, to = (16 * blk + i * C::RPL) * C::RB;
+        if constexpr (C::SHARED) load_rows(rk, p.k.token, dst + to, r, (lane % C::CH) ^ C::swizzle_k(r));
+        load_rows(rv, p.v.token, dst + C::V_AT + to, r, (lane % C::CH) ^ C::swizzle_v(r + 16 * blk));
+      }
+    }
+  }
+  // Requests the K rows [j0, j0 + KT) into registers: lane l has 16 bytes from 64 x + 16 (l / 16) on of row l mod 16 of
+  // each block. FP8: they are 16 elements, half for one product step and half for the next (q is laid out alike).
+  __device__ __forceinline__ void request_k(int32_t j0, u32x4 (&k)[C::KT / 16][C::KL]) {
+#pragma unroll
+    for (int bl = 0; bl < C::KT / 16; ++bl) {
+      const Rsrc r = rows_of(p.k, head_k, where(j0 + 16 * bl));
+#pragma unroll
+      for (int x = 0; x < C::KL; ++x) {
+        const uint32_t at = 64 * x + 16 * (lane >> 4);
+        k[bl][x] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                 r, at < p.D * C::ES ? (lane & 15) * p.k.token + at : 0x7fffffffu, 0, 0));
       }
     }
   }
@@ -209,7 +267,7 @@ struct Tiles {
 #pragma unroll
       for (int i = 0; i < 16 / C::RPL; ++i) {
         const int blk = C::SHARED ? wave : bl;
-        u32x4* src = reinterpret_cast<u32x4*>(buf + at * 2 * C::TILE + C::TILE + (16 * blk + i * C::RPL) * C::RB + lane * 16);
+        u32x4* src = reinterpret_cast<u32x4*>(buf + at * C::BUF + C::V_AT + (16 * blk + i * C::RPL) * C::RB + lane * 16);
         u32x4 u = *src;
         bool bad = false;
 #pragma unroll
@@ -230,34 +288,39 @@ struct Tiles {
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): written before the barrier
     return any;
   }
+  // What a lane reads for an operand; FP8 codes are widened where the operand is used, not where it is read.
+  using Raw = typename RawOf<C::FP8>::T;
+  __device__ static __forceinline__ bf16x8 operand(Raw w) {
+    if constexpr (C::FP8) return widen(w);
+    else return __builtin_bit_cast(bf16x8, w);
+  }
   // A operand of S^T: 16 keys from row 16 kb, elements 32 step .. + 31.
-  __device__ __forceinline__ bf16x8 k_frag(int at, int kb, int step) const {
+  __device__ __forceinline__ Raw k_frag(int at, int kb, int step) const {
     const int r = lane & 15, g = lane >> 4;
-    const unsigned char* row = buf + at * 2 * C::TILE + (16 * kb + r) * C::RB;
+    const unsigned char* row = buf + at * C::BUF + (16 * kb + r) * C::RB;
     if constexpr (C::FP8) {
       const int c = 2 * step + (g >> 1);
-      return widen(*reinterpret_cast<const i32x2*>(row + ((c ^ C::swizzle_k(r)) * 16) + (g & 1) * 8));
+      return *reinterpret_cast<const i32x2*>(row + ((c ^ C::swizzle_k(r)) * 16) + (g & 1) * 8);
     } else {
       const int c = 4 * step + g;
-      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(row + (c ^ C::swizzle_k(r)) * 16));
+      return *reinterpret_cast<const u32x4*>(row + (c ^ C::swizzle_k(r)) * 16);
     }
   }
   // A operand of O^T: elements 16 db .. + 15 of 32 keys from row 32 kc; k slot 8 g + e is key 4 g + e (e < 4), or
   // 16 + 4 g + e - 4.
-  __device__ __forceinline__ bf16x8 v_frag(int at, int kc, int db) const {
+  __device__ __forceinline__ Raw v_frag(int at, int kc, int db) const {
     const int i = lane & 15, g = lane >> 4;
-    unsigned char* tile = buf + at * 2 * C::TILE + C::TILE + 32 * kc * C::RB;
+    unsigned char* tile = buf + at * C::BUF + C::V_AT + 32 * kc * C::RB;
+    const unsigned char* filling = buf + (at ^ 1) * C::BUF;
     if constexpr (C::FP8) {
       const int j = i >> 1, r = j < 4 ? 4 * g + j : 12 + 4 * g + j;
       unsigned char* src = tile + r * C::RB + (db ^ C::swizzle_v(r)) * 16 + (i & 1) * 8;
-      return widen(__builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(src)));
+      return read_tr8(src, filling);
     } else {
       const int r = 4 * g + (i >> 2);
       unsigned char* src = tile + r * C::RB + ((2 * db + ((i >> 1) & 1)) ^ C::swizzle_v(r)) * 16 + (i & 1) * 8;
-      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src));
-      const s16x4 b =
-          __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src + 16 * C::RB));
-      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+      const s16x4 a = read_tr16(src, filling), b = read_tr16(src + 16 * C::RB, filling);
+      return __builtin_bit_cast(u32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     }
   }
   // Eight e4m3fn codes as bf16, exactly.
@@ -285,9 +348,11 @@ struct Rows {
   int32_t lo[C::CB], hi[C::CB]; // the keys that the row sees
 };
 
-// One tile of keys j0 .. j0 + KT - 1 for one wavefront's rows. masked: some row does not see some of them.
-template <class C>
-__device__ __forceinline__ void tile_step(const Tiles<C>& t, Rows<C>& w, int at, int32_t j0, float c, bool masked) {
+// One tile of keys j0 .. j0 + KT - 1 for one wavefront's rows. masked: some row does not see some of them. k_used is
+// called when the K rows are not needed any more.
+template <class C, class F>
+__device__ __forceinline__ void tile_step(const Tiles<C>& t, Rows<C>& w, const u32x4 (&kr)[C::KT / 16][C::KL], int at,
+                                          int32_t j0, float c, bool masked, F k_used) {
   constexpr int KB = C::KT / 16, KC = C::KT / 32, ND = C::DT / 16, NS = C::DT / 32;
   const int g = t.lane >> 4;
   f32x4 s[KB][C::CB];
@@ -295,19 +360,33 @@ __device__ __forceinline__ void tile_step(const Tiles<C>& t, Rows<C>& w, int at,
   for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
     for (int cb = 0; cb < C::CB; ++cb) s[kb][cb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  // one operand ahead of the products, no more: left to itself the compiler reads them all first and runs out of
+  // AHEAD operands ahead of the products, no more: left to itself the compiler reads them all first and runs out of
   // registers
-  bf16x8 a[2];
-  a[0] = t.k_frag(at, 0, 0);
+  constexpr int AHEAD = C::AHEAD, RING = AHEAD + 1;
+  typename Tiles<C>::Raw a[RING];
+  if constexpr (C::SHARED) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) a[i] = t.k_frag(at, i % KB, i / KB);
+  }
 #pragma unroll
   for (int i = 0; i < NS * KB; ++i) {
-    const int step = i / KB, kb = i % KB;
-    if (i + 1 < NS * KB) a[(i + 1) & 1] = t.k_frag(at, (i + 1) % KB, (i + 1) / KB);
+    const int step = i / KB, kb = i % KB, n = i + AHEAD;
+    bf16x8 f;
+    if constexpr (C::SHARED) {
+      if (n < NS * KB) a[n % RING] = t.k_frag(at, n % KB, n / KB);
+      f = Tiles<C>::operand(a[i % RING]);
+    } else if constexpr (C::FP8) {
+      const u32x4 u = kr[kb][step / 2];
+      f = Tiles<C>::widen(i32x2{static_cast<int>(u[2 * (step % 2)]), static_cast<int>(u[2 * (step % 2) + 1])});
+    } else {
+      f = __builtin_bit_cast(bf16x8, kr[kb][step]);
+    }
 #pragma unroll
     for (int cb = 0; cb < C::CB; ++cb)
-      s[kb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i & 1], w.q[step][cb], s[kb][cb], 0, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
+      s[kb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, w.q[step][cb], s[kb][cb], 0, 0, 0);
+    if constexpr (C::SHARED) __builtin_amdgcn_sched_barrier(0);
   }
+  k_used();
 
   if (masked) {
 #pragma unroll
@@ -352,6 +431,8 @@ __device__ __forceinline__ void tile_step(const Tiles<C>& t, Rows<C>& w, int at,
     }
   }
 
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) a[i] = t.v_frag(at, i / ND, i % ND);
   // weights, their sums, and the operand of the second product
   bf16x8 pf[KC][C::CB];
 #pragma unroll
@@ -371,14 +452,14 @@ __device__ __forceinline__ void tile_step(const Tiles<C>& t, Rows<C>& w, int at,
       }
   }
 
-  a[0] = t.v_frag(at, 0, 0);
 #pragma unroll
   for (int i = 0; i < KC * ND; ++i) {
-    const int kc = i / ND, db = i % ND;
-    if (i + 1 < KC * ND) a[(i + 1) & 1] = t.v_frag(at, (i + 1) / ND, (i + 1) % ND);
+    const int kc = i / ND, db = i % ND, n = i + AHEAD;
+    if (n < KC * ND) a[n % RING] = t.v_frag(at, n / ND, n % ND);
+    const bf16x8 f = Tiles<C>::operand(a[i % RING]);
 #pragma unroll
     for (int cb = 0; cb < C::CB; ++cb)
-      w.o[db][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i & 1], pf[kc][cb], w.o[db][cb], 0, 0, 0);
+      w.o[db][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pf[kc][cb], w.o[db][cb], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   }
 }
@@ -410,25 +491,113 @@ __device__ __forceinline__ void add_infinities(const Tiles<C>& t, Rows<C>& w, in
   }
 }
 
-// The sequence that row tile `idx` of the grid belongs to. Sequence b's tiles begin at q_start[b] G / BM + b: that
-// leaves each at least the tiles it needs. 64 lanes probe at once: one round for up to 64 sequences.
-template <int BM>
-__device__ __forceinline__ int find_sequence(const Params& p, int lane, int32_t idx) {
-  int lo = 0;
-  int64_t step = 1;
-  while (step * 64 < p.batch) step *= 64;
-  for (; step > 0; step /= 64) {
-    const int64_t b = lo + lane * step;
-    bool before = false;
-    if (b < p.batch) {
-      int32_t q0 = p.q_start[b];
-      q0 = q0 < 0 ? 0 : q0 > p.T ? static_cast<int32_t>(p.T) : q0;
-      before = static_cast<int64_t>(q0) * p.group.d / BM + b <= idx;
+// x plus what another lane has (lanes without a source: plus 0).
+template <int CTRL, int ROWS, class T>
+__device__ __forceinline__ T add_from(T x) {
+  return x + __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, ROWS, 0xf, false));
+}
+// Inclusive sums over the lanes.
+template <class T>
+__device__ __forceinline__ T lane_sums(T x) {
+  x = add_from<0x111, 0xf>(x);  // 1, 2, 4, 8 lanes back in the row of 16
+  x = add_from<0x112, 0xf>(x);
+  x = add_from<0x114, 0xf>(x);
+  x = add_from<0x118, 0xf>(x);
+  x = add_from<0x142, 0xa>(x);     // the end of row 0 (2) into row 1 (3)
+  return add_from<0x143, 0xc>(x);  // the end of row 1 into rows 2 and 3
+}
+template <class T>
+__device__ __forceinline__ T last_lane(T x) {
+  return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+
+// A sequence as the kernels see it, whatever its arrays hold.
+struct Sequence {
+  int32_t q0, n, m;  // first token, new tokens, cached tokens
+};
+__device__ __forceinline__ Sequence sequence(const Params& p, int b) {
+  const int32_t T = static_cast<int32_t>(p.T);
+  int32_t q0 = p.q_start[b], q1 = p.q_start[b + 1], m = p.kv_len[b];
+  q0 = q0 < 0 ? 0 : q0 > T ? T : q0;
+  q1 = q1 < q0 ? q0 : q1 > T ? T : q1;
+  const int64_t most = p.ld_table << p.page_shift;
+  m = m < 0 ? 0 : m > most ? static_cast<int32_t>(most) : m;
+  return Sequence{q0, q1 - q0, m};
+}
+
+// What a workgroup does: a row tile of a sequence and a part of its keys.
+struct Item {
+  int32_t b, tile, part, parts, per;  // per: key steps of a part
+  Sequence s;
+};
+
+// Deals the sequences' row tiles and parts to the p.items workgroups of a KV head. A part has `per` key steps, the
+// same for all sequences, the least with which the parts are no more than the workgroups: workgroups take equally
+// long whatever the sequences' lengths. Every wavefront finds the same from q_start and kv_len, a lane for a sequence.
+// False: nothing left for workgroup `idx`.
+template <class C>
+__device__ __forceinline__ bool schedule(const Params& p, int lane, int32_t idx, Item& it) {
+  const int32_t G = static_cast<int32_t>(p.group.d);
+  struct Need {
+    int32_t tiles, steps;
+  };
+  Sequence mine{0, 0, 0};
+  const auto need = [&](int base) {
+    mine = base + lane < p.batch ? sequence(p, base + lane) : Sequence{0, 0, 0};
+    int32_t keys = mine.m;
+    if (p.window) {  // a row tile's rows see a window and the tokens that they span
+      const int32_t span = (C::BM + G - 2) / G + 1, most = p.window < 0x7fffffff - span ? p.window + span : 0x7fffffff;
+      keys = keys < most ? keys : most;
     }
-    const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(before));
-    lo += static_cast<int>((n ? n - 1 : 0) * step);
+    return Need{(mine.n * G + C::BM - 1) / C::BM, (keys + C::STEP - 1) / C::STEP + (p.window ? 1 : 0)};
+  };
+  const auto parts = [](const Need& x, int32_t per) { return x.steps > per ? (x.steps + per - 1) / per : 1; };
+  Need x = need(0);
+  int32_t per = 0x7fffffff, count = 0;  // not split
+  if (p.part_o) {
+    float work = 0.0f;
+    for (int base = 0; base < p.batch; base += 64) {
+      if (base) x = need(base);
+      work += last_lane(lane_sums(static_cast<float>(x.tiles) * static_cast<float>(x.steps)));
+    }
+    per = static_cast<int32_t>(work / static_cast<float>(p.items));
+    per = per < p.min_part ? p.min_part : per;
+    if (p.batch > 64) x = need(0);
   }
-  return lo;
+  while (true) {
+    count = 0;
+    for (int base = 0; base < p.batch; base += 64) {
+      if (base) x = need(base);
+      count += last_lane(lane_sums(x.tiles * parts(x, per)));
+    }
+    if (p.batch > 64) x = need(0);
+    // with one part each the tiles of any ascending q_start are no more than the workgroups
+    if (count <= p.items || per >= 1 << 30) break;
+    const int32_t more = per / 16;
+    per += more < 1 ? 1 : more;
+  }
+  // later tiles, which see more keys where causal, come first
+  int32_t left = count - 1 - idx;
+  if (left < 0) return false;
+  for (int base = 0; base < p.batch; base += 64) {
+    if (base) x = need(base);
+    const int32_t own = x.tiles * parts(x, per), upto = lane_sums(own);
+    const uint64_t after = __builtin_amdgcn_ballot_w64(upto > left);
+    if (after) {
+      const int at = __builtin_ctzll(after);
+      const auto of = [&](int32_t v) { return __builtin_amdgcn_readlane(v, at); };
+      it.b = base + at;
+      it.parts = of(parts(x, per));
+      it.per = per;
+      const int32_t in = left - (of(upto) - of(own));
+      it.tile = in / it.parts;
+      it.part = in - it.tile * it.parts;
+      it.s = Sequence{of(mine.q0), of(mine.n), of(mine.m)};
+      return true;
+    }
+    left -= last_lane(upto);
+  }
+  return false;  // not reached
 }
 
 template <class C>
@@ -439,27 +608,14 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
   const int lane = static_cast<int>(threadIdx.x) & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
 
-  // which rows: consecutive workgroups take the KV heads in turn (on 8 XCDs a head's keys then stay in few L2s);
-  // later row tiles, which see more keys where causal, come first
-  const uint32_t bid = blockIdx.x;
-  const uint32_t rest = div(bid, p.kv_heads);
-  const int head = static_cast<int>(bid - rest * p.kv_heads.d);
-  const uint32_t order = div(rest, p.splits);
-  const int split = static_cast<int>(rest - order * p.splits.d);
-  const int32_t idx = p.tiles - 1 - static_cast<int32_t>(order);
-  const int b = find_sequence<C::BM>(p, lane, idx);
-  const int32_t T = static_cast<int32_t>(p.T);
-  int32_t q0 = p.q_start[b], q1 = p.q_start[b + 1];
-  q0 = q0 < 0 ? 0 : q0 > T ? T : q0;
-  q1 = q1 < q0 ? q0 : q1 > T ? T : q1;
-  const int32_t G = static_cast<int32_t>(p.group.d), n = q1 - q0, R = n * G;
-  const int32_t row0 = (idx - static_cast<int32_t>(static_cast<int64_t>(q0) * G / C::BM) - b) * C::BM;
-  if (row0 < 0 || row0 >= R) return;
-  int32_t m = p.kv_len[b];
-  {
-    const int64_t most = p.ld_table << p.page_shift;
-    m = m < 0 ? 0 : m > most ? static_cast<int32_t>(most) : m;
-  }
+  // consecutive workgroups take the KV heads in turn: on 8 XCDs a head's keys then stay in few L2s
+  const uint32_t bid = blockIdx.x, idx = div(bid, p.kv_heads);
+  const int head = static_cast<int>(bid - idx * p.kv_heads.d);
+  Item it;
+  if (!schedule<C>(p, lane, static_cast<int32_t>(idx), it)) return;
+  const int b = it.b;
+  const int32_t q0 = it.s.q0, n = it.s.n, m = it.s.m, G = static_cast<int32_t>(p.group.d), R = n * G;
+  const int32_t row0 = it.tile * C::BM;
 
   // keys that the rows first .. last see
   const int32_t ahead = m - n;  // position of the first new token
@@ -479,12 +635,11 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
   };
   const int32_t row_end = row0 + C::BM < R ? row0 + C::BM : R;
   const Range all = range(row0, row_end - 1);
-  // key tiles of the whole workgroup and of this split
-  const int32_t tile0 = all.lo / C::KT, tiles = all.hi > all.lo ? (all.hi + C::KT - 1) / C::KT - tile0 : 0;
-  int32_t per = (tiles + static_cast<int32_t>(p.splits.d) - 1) / static_cast<int32_t>(p.splits.d);
-  if (per < p.min_tiles) per = p.min_tiles;
-  const int32_t first = split * per, count = tiles - first < per ? tiles - first : per;
-  const int32_t j_begin = (tile0 + first) * C::KT;
+  // key steps of the row tile and of this part
+  const int32_t step0 = all.lo / C::STEP, steps = all.hi > all.lo ? (all.hi + C::STEP - 1) / C::STEP - step0 : 0;
+  const int32_t first = it.part * it.per;  // one part: 0
+  const int32_t rest = steps - first, mine = rest < 0 ? 0 : it.part == it.parts - 1 || rest < it.per ? rest : it.per;
+  const int32_t j_begin = (step0 + first) * C::STEP, count = mine * (C::STEP / C::KT);
 
   // rows of this wavefront
   const int32_t w0 = row0 + (C::SHARED ? wave * 16 * C::CB : 0);
@@ -510,7 +665,8 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
     const uint16_t* src = p.q + at_t[cb] * p.ldq + static_cast<int64_t>(at_h[cb]) * p.D;
 #pragma unroll
     for (int step = 0; step < NS; ++step) {
-      const int d = 32 * step + 8 * (lane >> 4);
+      // the elements that K's operand has there (request_k)
+      const int d = !C::SHARED && C::FP8 ? 64 * (step / 2) + 16 * (lane >> 4) + 8 * (step % 2) : 32 * step + 8 * (lane >> 4);
       u32x4 u = {0u, 0u, 0u, 0u};
       if (d < p.D) u = *reinterpret_cast<const u32x4*>(src + d);
       w.q[step][cb] = __builtin_bit_cast(bf16x8, u);
@@ -526,15 +682,16 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
   const float k_scale = p.k.scale ? p.k.scale[head] : 1.0f, v_scale = p.v.scale ? p.v.scale[head] : 1.0f;
   const float c = p.c * k_scale;
   const auto in_part = [&](int32_t j0) { return j0 < inner.lo || j0 + C::KT > inner.hi; };
-  const auto step = [&](const Tiles<C>& t, int at, int32_t j0) {
-    if (!busy || j0 >= any.hi || j0 + C::KT <= any.lo) return;
-    tile_step(t, w, at, j0, c, j0 < full.lo || j0 + C::KT > full.hi);
+  u32x4 kr[C::KT / 16][C::KL];
+  const auto step = [&](const Tiles<C>& t, int at, int32_t j0, auto&& k_used) {
+    if (C::SHARED && (!busy || j0 >= any.hi || j0 + C::KT <= any.lo)) return;
+    tile_step(t, w, kr, at, j0, c, j0 < full.lo || j0 + C::KT > full.hi, k_used);
   };
 
   if (threadIdx.x == 0) any_infinite = 0;
   __syncthreads();
   if (count > 0) {
-    Tiles<C> t(p, lds + (C::SHARED ? 0 : wave * 4 * C::TILE), lane, wave);
+    Tiles<C> t(p, lds + (C::SHARED ? 0 : wave * 2 * C::BUF), lane, wave);
     t.open(b, head, m, j_begin);
     if constexpr (C::SHARED) {
       t.request(j_begin, 0);
@@ -544,21 +701,28 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
         if (in_part(j0) && t.make_finite(i & 1)) any_infinite = 1;
         group_barrier();   // every wavefront's are, and all have read tile i - 1
         if (i + 1 < count) t.request(j0 + C::KT, (i + 1) & 1);
-        step(t, i & 1, j0);
+        step(t, i & 1, j0, [] {});
       }
     } else {
-      if (wave < count) t.request(j_begin + wave * C::KT, 0);
+      if (wave < count) {
+        t.request(j_begin + wave * C::KT, 0);
+        t.request_k(j_begin + wave * C::KT, kr);
+      }
       int at = 0;
       for (int32_t i = wave; i < count; i += C::WAVES, at ^= 1) {
-        const int32_t j0 = j_begin + i * C::KT;
-        if (i + C::WAVES < count) {
-          t.request(j0 + C::WAVES * C::KT, at ^ 1);
-          wait_loads<C::LOADS>();
+        const int32_t j0 = j_begin + i * C::KT, j1 = j0 + C::WAVES * C::KT;
+        const bool more = i + C::WAVES < count;
+        if (more) {
+          t.request(j1, at ^ 1);
+          wait_loads<C::V_LOADS>();  // all but those: this tile's
         } else {
           wait_loads<0>();
         }
         if (in_part(j0) && t.make_finite(at)) any_infinite = 1;
-        step(t, at, j0);
+        // the next K rows take the registers as soon as the scores are there
+        step(t, at, j0, [&] {
+          if (more) t.request_k(j1, kr);
+        });
         asm volatile("" ::: "memory");  // the next request writes where this tile was read
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -576,10 +740,14 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
     w.l[cb] += __shfl_xor(w.l[cb], 16);
     w.l[cb] += __shfl_xor(w.l[cb], 32);
   }
-  const bool whole = p.splits.d == 1;
-  const auto put = [&](int64_t tok, int32_t h, int d, f32x4 o, float bound, float sum, bool first_lane) {
-    // bound in log2 units; o, sum relative to it
+  const bool whole = it.parts == 1;
+  const auto put = [&](int32_t i, int64_t tok, int32_t h, int d, f32x4 o, float bound, float sum, bool first_lane) {
+    // row i of the tile; bound in log2 units; o, sum relative to it
     const int64_t r = tok * p.n_q + h;
+    if (first_lane && p.part_o && it.part == 0) {  // the next part is p.n_kv workgroups before this one
+      p.parts_of[r][0] = static_cast<int32_t>(bid);
+      p.parts_of[r][1] = it.parts * 256 + i;
+    }
     if (whole) {
       const float f = sum == 0.0f ? 0.0f : v_scale / sum;
       if (d < p.D) {
@@ -588,7 +756,7 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
       }
       if (first_lane && p.lse) p.lse[r] = sum == 0.0f ? neg_inf() : (bound + __builtin_amdgcn_logf(sum)) * kLn2;
     } else {
-      const int64_t at = split * p.T * p.n_q + r;
+      const int64_t at = static_cast<int64_t>(bid) * C::BM + i;
       if (d < p.D && sum != 0.0f) {
         const f32x4 x = {o[0] * v_scale, o[1] * v_scale, o[2] * v_scale, o[3] * v_scale};
         *reinterpret_cast<f32x4*>(p.part_o + at * p.D + d) = x;
@@ -602,7 +770,7 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
       if (row[cb] < R)
 #pragma unroll
         for (int db = 0; db < ND; ++db)
-          put(at_t[cb], at_h[cb], 16 * db + 4 * (lane >> 4), w.o[db][cb], w.m[cb] * c, w.l[cb], db == 0 && lane < 16);
+          put(row[cb] - row0, at_t[cb], at_h[cb], 16 * db + 4 * (lane >> 4), w.o[db][cb], w.m[cb] * c, w.l[cb], db == 0 && lane < 16);
   } else {
     // join the wavefronts, in ascending order: rows of (DT + 4) floats, then bounds, then sums
     float* rows = reinterpret_cast<float*>(lds);
@@ -640,14 +808,14 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
         for (int e = 0; e < 4; ++e) o[e] += f * v[e];
       }
       const int32_t tok = static_cast<int32_t>(div(r, p.group));
-      put(q0 + tok, head * G + r - tok * G, d, o, top, sum, d == 0);
+      put(i, q0 + tok, head * G + r - tok * G, d, o, top, sum, d == 0);
     }
   }
 }
 
 template <class C>
 Variant variant(const char* name) {
-  return Variant{reinterpret_cast<const void*>(&qkn_attn_kernel<C>), C::BM, C::KT * C::STAGES, 64 * C::WAVES, C::LDS, name};
+  return Variant{reinterpret_cast<const void*>(&qkn_attn_kernel<C>), C::BM, C::STEP, 64 * C::WAVES, C::LDS, C::SLOTS, name};
 }
 
 // A kernel for sequences of up to `rows` rows, and one for more. dt: 64, 128 or 256.
