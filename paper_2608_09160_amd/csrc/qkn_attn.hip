@@ -79,24 +79,20 @@ __global__ __launch_bounds__(kJoinThreads) void qkn_attn_join(const Params p, in
 }
 
 constexpr int64_t kJoinFew = 4096;  // rows
-
-#ifndef V_SLOTS
-#define V_SLOTS 1
-#endif
-#ifndef V_MINF
-#define V_MINF 4
-#endif
-#ifndef V_MINM
-#define V_MINM 4
-#endif
-constexpr int kRounds = V_SLOTS;
-constexpr int kMinPartFew = V_MINF, kMinPartMany = V_MINM;  // key steps of a part, at least
+// Key steps of a part, at least (few rows: 128 keys each, many: 64): a part costs a workgroup's start and a share of the
+// join (4 single tokens over up to 500 keys, D 128: 9.4 us whole, 11.6 in parts of two steps).
+constexpr int kMinPart = 4;
+// Pairs of 64 rows and 64 keys up to which many-row launches take 64 rows to a workgroup (16 + 4 heads of 128, us with 64
+// and with 128 rows: prompts of 256 tokens 9.6 and 12.2, 1024 21.7 and 26.6, 2048 39.1 and 49.7, 8192 344 and 277; 128
+// tokens behind 8064 24.9 and 26.7, 512 behind 7680 54.1 and 49.9; 16 + 2 heads of 64, 12 chunks of up to 512 tokens,
+// window 1024, 26.0 and 29.6). They need more LDS reads for the same products, but
+// make more workgroups.
+constexpr int64_t kSmallPairs = 12288;
 
 struct Plan {
   Variant v;
   int64_t items, grid;              // workgroups of a KV head, of the launch
   int64_t o_bytes, ml_bytes, ws_bytes;
-  int min_part;
   bool split;
 };
 
@@ -122,14 +118,25 @@ Plan plan_of(const qkn_attn_args& a, const qkn_cache& c) {
   const int dt = c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256;
   const int64_t group = a.n_q / c.n_kv, rows = (a.max_q < 1 ? 1 : a.max_q) * group;
   const bool few = rows <= (dt == 256 ? 32 : 64);
-  pl.v = few ? few_rows(dt, c.fp8 != 0, static_cast<int>(rows)) : many_rows(dt, c.fp8 != 0);
+  if (few) {
+    pl.v = few_rows(dt, c.fp8 != 0, static_cast<int>(rows));
+  } else {
+    // keys that a row sees, about, and pairs of 64 rows and 64 keys in all
+    int64_t keys = a.max_kv - (a.causal ? (a.max_q < a.max_kv ? a.max_q : a.max_kv) / 2 : 0);
+    if (a.window && a.window < keys) keys = a.window;
+    const int64_t pairs = (a.T * group + 63) / 64 * c.n_kv * ((keys + 63) / 64);
+    pl.v = many_rows(dt, c.fp8 != 0, pairs <= kSmallPairs);
+  }
   pl.items = a.T * group / pl.v.rows + a.batch;  // the most row tiles that T tokens can make
-  const int64_t slots = int64_t{kRounds} * pl.v.slots * kCus / c.n_kv;
-  pl.min_part = few ? kMinPartFew : kMinPartMany;
-  pl.split = pl.items < slots && a.max_kv > int64_t{pl.min_part} * pl.v.step;
+  const int64_t slots = int64_t{pl.v.slots} * kCus / c.n_kv;
+  // Split keys to fill the chip once, not more (two rounds of half the parts: 40.4 against 34.6 us for 64 single tokens
+  // over up to 4096 keys), and not for less than a doubling (12 chunks of up to 512 tokens, window 1024: 41.7 split,
+  // 29.7 us whole).
+  const int64_t part = int64_t{kMinPart} * pl.v.step;
+  pl.split = 2 * pl.items <= slots && a.max_kv > part;
   if (pl.split) {
     // the workgroups that take turns on the chip, or as many as the keys can use
-    const int64_t most = pl.items * ((a.max_kv + int64_t{pl.min_part} * pl.v.step - 1) / (int64_t{pl.min_part} * pl.v.step));
+    const int64_t most = pl.items * ((a.max_kv + part - 1) / part);
     pl.items = slots < most ? slots : most;
     pl.ml_bytes = pl.items * c.n_kv * pl.v.rows * 8;
     pl.o_bytes = pl.items * c.n_kv * pl.v.rows * 4 * int64_t{c.head_dim};
@@ -205,7 +212,7 @@ int attn_impl(const qkn_attn_args* args, const qkn_cache* cache, void* workspace
   p.c = a.scale * 1.44269504088896340736f;
   p.group = fast_div(static_cast<uint32_t>(a.n_q / c.n_kv));
   p.kv_heads = fast_div(static_cast<uint32_t>(c.n_kv));
-  p.min_part = pl.min_part;
+  p.min_part = kMinPart;
   if (pl.split) {
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     p.part_o = reinterpret_cast<float*>(ws);

@@ -112,10 +112,7 @@ template <int DT_, bool FP8_, int CB_, int WAVES_, bool SHARED_, int KT_, int OC
 struct Cfg {
   static constexpr int DT = DT_, CB = CB_, WAVES = WAVES_, KT = KT_, OCC = OCC_;
   static constexpr bool FP8 = FP8_, SHARED = SHARED_;
-#ifndef QKN_AHEAD
-#define QKN_AHEAD 2
-#endif
-  static constexpr int AHEAD = QKN_AHEAD;
+  static constexpr int AHEAD = 4;                 // LDS reads ahead of their products
   static constexpr int ES = FP8 ? 1 : 2;
   static constexpr int RB = DT * ES;              // bytes of an LDS row
   static constexpr int CH = RB / 16;              // its 16-byte chunks
@@ -127,15 +124,16 @@ struct Cfg {
   static constexpr int V_AT = SHARED ? TILE : 0;  // V in it
   static constexpr int STEP = KT * (SHARED ? 1 : WAVES);  // keys that a workgroup takes at a time
   static constexpr int KL = DT * ES / 64;         // 16-byte loads of 16 K rows into registers (!SHARED)
-  static constexpr int BLOCKS = SHARED ? KT / 16 / WAVES : KT / 16;  // 16-row blocks that a wavefront loads
-  static constexpr int V_LOADS = BLOCKS * 16 / RPL;  // load instructions of a wavefront for a V tile
+  static constexpr int BR = SHARED ? KT / WAVES : 16;  // rows that a wavefront loads together, of one page
+  static constexpr int BLOCKS = SHARED ? 1 : KT / 16;  // how often for a tile
+  static constexpr int V_LOADS = BLOCKS * BR / RPL;    // load instructions of a wavefront for a V tile
   static constexpr int STAGES = SHARED ? 1 : WAVES;    // key streams of a workgroup
   static constexpr int JOIN_ROW = DT + 4;         // floats of a row while wavefronts are joined
   static constexpr int JOIN = SHARED ? 0 : WAVES * 16 * CB * (JOIN_ROW + 2) * 4;
   static constexpr int LDS = 2 * BUF * STAGES > JOIN ? 2 * BUF * STAGES : JOIN;
-  static_assert(!SHARED || KT == 16 * WAVES, "a block of 16 rows for every wavefront");
-  static constexpr int SLOTS = OCC < 160 * 1024 / LDS ? OCC : 160 * 1024 / LDS;  // workgroups that a CU holds
+  static_assert(BR % RPL == 0, "whole load instructions");
   static_assert(WAVES == 4, "a wavefront of a workgroup on each SIMD");
+  static constexpr int SLOTS = OCC < 160 * 1024 / LDS ? OCC : 160 * 1024 / LDS;  // workgroups that a CU holds
   static_assert(LDS <= 160 * 1024, "LDS");
   static_assert(CH <= 64 && V_LOADS < 64, "loads");
   // Chunk c of row r is stored at c ^ swizzle(r). K: 16 lanes read the same chunk of 16 rows.
@@ -178,12 +176,14 @@ struct Tiles {
   unsigned char* buf;       // its stream's two buffers
   int lane, wave;
   const Params& p;
-  int64_t head_k, head_v;   // bytes to the head
+  const unsigned char* base_k;  // the head's rows of page 0
+  const unsigned char* base_v;
   int32_t kv_len;
   const int32_t* table;     // the sequence's pages
   int32_t last_page;        // last entry in use
-  int32_t page0;            // pages held: lane i has entry page0 + i, then page0 + 64 + i
-  int32_t cur, next;
+  int32_t page0;            // pages held: lane i has the bytes to page entry page0 + i (lower, upper half; < 0: none)
+  int32_t k_lo, k_hi, v_lo, v_hi;
+  int32_t next;             // and entry page0 + 64 + i
 
   __device__ __forceinline__ Tiles(const Params& pp, unsigned char* b, int l, int w) : buf(b), lane(l), wave(w), p(pp) {}
 
@@ -191,55 +191,61 @@ struct Tiles {
     i = i < last_page ? i : last_page;
     return table[i < 0 ? 0 : i];
   }
+  // Takes 64 pages' places at once, a lane each: the address of a tile is then a few scalar instructions.
+  __device__ __forceinline__ void hold(int32_t page) {
+    const bool none = static_cast<uint32_t>(page) >= p.num_pages;
+    const int64_t k = none ? -1 : page * p.k.page, v = none ? -1 : page * p.v.page;
+    k_lo = static_cast<int32_t>(k);
+    k_hi = static_cast<int32_t>(k >> 32);
+    v_lo = static_cast<int32_t>(v);
+    v_hi = static_cast<int32_t>(v >> 32);
+  }
   __device__ __forceinline__ void open(int b, int head, int32_t m, int32_t first_key) {
-    head_k = head * p.k.head;
-    head_v = head * p.v.head;
+    base_k = p.k.base + head * p.k.head;
+    base_v = p.v.base + head * p.v.head;
     kv_len = m;
     table = p.table + b * p.ld_table;
     last_page = (m - 1) >> p.page_shift;
     page0 = first_key >> p.page_shift;
-    cur = entry(page0 + lane);
+    const int32_t first = entry(page0 + lane);
     next = entry(page0 + 64 + lane);
+    hold(first);
   }
-  // The 16 rows from key j on: page, row in it, and how many of them the sequence has.
-  struct Where {
-    int64_t page, row0;
-    uint32_t rows;
-  };
-  __device__ __forceinline__ Where where(int32_t j) {
+  // The BR rows of K (V) from key j on, which are in one page: a descriptor of those that the sequence has.
+  template <bool V>
+  __device__ __forceinline__ Rsrc rows_of(int32_t j) {
     const int32_t pi = j >> p.page_shift;
     while (pi - page0 >= 64) {  // pages are taken in ascending order
-      cur = next;
+      hold(next);
       page0 += 64;
       next = entry(page0 + 64 + lane);
     }
-    const int32_t page = __builtin_amdgcn_readlane(cur, pi - page0);
-    const int32_t left = kv_len - j;
-    const int32_t rows = static_cast<uint32_t>(page) >= p.num_pages ? 0 : left < 0 ? 0 : left < 16 ? left : 16;
-    return Where{rows ? page : 0, j & ((1 << p.page_shift) - 1), static_cast<uint32_t>(rows)};
+    const int32_t lo = __builtin_amdgcn_readlane(V ? v_lo : k_lo, pi - page0);
+    const int32_t hi = __builtin_amdgcn_readlane(V ? v_hi : k_hi, pi - page0);
+    const uint32_t token = V ? p.v.token : p.k.token, row0 = j & ((1 << p.page_shift) - 1);
+    const int32_t left = kv_len - j, rows = left < C::BR ? left : C::BR;
+    const bool none = left <= 0 || hi < 0;
+    const uint64_t off = (static_cast<uint64_t>(static_cast<uint32_t>(hi)) << 32 | static_cast<uint32_t>(lo)) +
+                         static_cast<uint64_t>(row0 * token);
+    // a scalar, as it is the same on all lanes: a descriptor in vector registers costs a loop around every load
+    const uint32_t bytes = __builtin_amdgcn_readfirstlane(none ? 0 : rows * token - (token - p.D * C::ES));
+    return rsrc((V ? base_v : base_k) + (none ? 0 : off), bytes);
   }
-  __device__ __forceinline__ Rsrc rows_of(const Pool& pool, int64_t head, const Where& w) const {
-    // scalars, as they are the same on all lanes: a descriptor in vector registers costs a loop around every load
-    const uint32_t bytes = __builtin_amdgcn_readfirstlane(w.rows ? w.rows * pool.token - (pool.token - p.D * C::ES) : 0);
-    return rsrc(pool.base + w.page * pool.page + head + w.row0 * pool.token, bytes);
-  }
-  // One load instruction's rows of a 16-row block into LDS.
-  __device__ __forceinline__ void load_rows(Rsrc r, uint32_t token, unsigned char* dst, int row, int chunk) {
-    load_to_lds(r, dst, chunk * 16 < p.D * C::ES ? row * token + chunk * 16 : 0x7fffffffu);
-  }
-  // Requests rows [j0, j0 + KT) (SHARED: this wavefront's 16 of them) into buffer `at`; !SHARED: V's only.
+  __device__ __forceinline__ int first_row(int bl) const { return C::BR * (C::SHARED ? wave : bl); }
+  // Requests this wavefront's rows of the K (V) tile at key j0 into buffer `at`.
+  template <bool V>
   __device__ __forceinline__ void request(int32_t j0, int at) {
-    unsigned char* dst = buf + at * C::BUF;
 #pragma unroll
     for (int bl = 0; bl < C::BLOCKS; ++bl) {
-      const int blk = C::SHARED ? wave : bl;
-      const Where w = where(j0 + 16 * blk);
-      const Rsrc rk = rows_of(p.k, head_k, w), rv = rows_of(p.v, head_v, w);
+      const int row0 = first_row(bl);
+      const Rsrc rs = rows_of<V>(j0 + row0);
+      const uint32_t token = V ? p.v.token : p.k.token;
+      unsigned char* dst = buf + at * C::BUF + (V ? C::V_AT : 0) + row0 * C::RB;
 #pragma unroll
-      for (int i = 0; i < 16 / C::RPL; ++i) {
-        const int r = i * C::RPL + lane / C::CH, to = (16 * blk + i * C::RPL) * C::RB;
-        if constexpr (C::SHARED) load_rows(rk, p.k.token, dst + to, r, (lane % C::CH) ^ C::swizzle_k(r));
-        load_rows(rv, p.v.token, dst + C::V_AT + to, r, (lane % C::CH) ^ C::swizzle_v(r + 16 * blk));
+      for (int i = 0; i < C::BR / C::RPL; ++i) {
+        const int r = i * C::RPL + lane / C::CH;
+        const int chunk = (lane % C::CH) ^ (V ? C::swizzle_v(row0 + r) : C::swizzle_k(row0 + r));
+        load_to_lds(rs, dst + i * C::RPL * C::RB, chunk * 16 < p.D * C::ES ? r * token + chunk * 16 : 0x7fffffffu);
       }
     }
   }
@@ -248,7 +254,7 @@ struct Tiles {
   __device__ __forceinline__ void request_k(int32_t j0, u32x4 (&k)[C::KT / 16][C::KL]) {
 #pragma unroll
     for (int bl = 0; bl < C::KT / 16; ++bl) {
-      const Rsrc r = rows_of(p.k, head_k, where(j0 + 16 * bl));
+      const Rsrc r = rows_of<false>(j0 + 16 * bl);
 #pragma unroll
       for (int x = 0; x < C::KL; ++x) {
         const uint32_t at = 64 * x + 16 * (lane >> 4);
@@ -265,9 +271,9 @@ struct Tiles {
 #pragma unroll
     for (int bl = 0; bl < C::BLOCKS; ++bl)
 #pragma unroll
-      for (int i = 0; i < 16 / C::RPL; ++i) {
-        const int blk = C::SHARED ? wave : bl;
-        u32x4* src = reinterpret_cast<u32x4*>(buf + at * C::BUF + C::V_AT + (16 * blk + i * C::RPL) * C::RB + lane * 16);
+      for (int i = 0; i < C::BR / C::RPL; ++i) {
+        u32x4* src =
+            reinterpret_cast<u32x4*>(buf + at * C::BUF + C::V_AT + (first_row(bl) + i * C::RPL) * C::RB + lane * 16);
         u32x4 u = *src;
         bool bad = false;
 #pragma unroll
@@ -348,14 +354,16 @@ struct Rows {
   int32_t lo[C::CB], hi[C::CB]; // the keys that the row sees
 };
 
-// One tile of keys j0 .. j0 + KT - 1 for one wavefront's rows. masked: some row does not see some of them. k_used is
-// called when the K rows are not needed any more.
-template <class C, class F>
-__device__ __forceinline__ void tile_step(const Tiles<C>& t, Rows<C>& w, const u32x4 (&kr)[C::KT / 16][C::KL], int at,
-                                          int32_t j0, float c, bool masked, F k_used) {
-  constexpr int KB = C::KT / 16, KC = C::KT / 32, ND = C::DT / 16, NS = C::DT / 32;
-  const int g = t.lane >> 4;
-  f32x4 s[KB][C::CB];
+template <class C>
+using Scores = f32x4[C::KT / 16][C::CB];
+template <class C>
+using Weights = bf16x8[C::KT / 32][C::CB];
+
+// S^T = K Q^T of the tile in buffer `at` (!SHARED: of the K rows in kr).
+template <class C>
+__device__ __forceinline__ void scores(const Tiles<C>& t, const Rows<C>& w, const u32x4 (&kr)[C::KT / 16][C::KL], int at,
+                                       Scores<C>& s) {
+  constexpr int KB = C::KT / 16, NS = C::DT / 32;
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -386,8 +394,15 @@ __device__ __forceinline__ void tile_step(const Tiles<C>& t, Rows<C>& w, const u
       s[kb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, w.q[step][cb], s[kb][cb], 0, 0, 0);
     if constexpr (C::SHARED) __builtin_amdgcn_sched_barrier(0);
   }
-  k_used();
+}
 
+// The scores of keys j0 .. j0 + KT - 1 to weights, with the rows' bounds and sums. masked: some row does not see some
+// of the keys.
+template <class C>
+__device__ __forceinline__ void softmax(Rows<C>& w, Scores<C>& s, Weights<C>& pf, int lane, int32_t j0, float c,
+                                        bool masked) {
+  constexpr int KB = C::KT / 16, KC = C::KT / 32, ND = C::DT / 16;
+  const int g = lane >> 4;
   if (masked) {
 #pragma unroll
     for (int cb = 0; cb < C::CB; ++cb) {
@@ -431,10 +446,7 @@ __device__ __forceinline__ void tile_step(const Tiles<C>& t, Rows<C>& w, const u
     }
   }
 
-#pragma unroll
-  for (int i = 0; i < AHEAD; ++i) a[i] = t.v_frag(at, i / ND, i % ND);
   // weights, their sums, and the operand of the second product
-  bf16x8 pf[KC][C::CB];
 #pragma unroll
   for (int cb = 0; cb < C::CB; ++cb) {
     const float shift = w.m[cb] == neg_inf() ? 0.0f : -w.m[cb] * c;
@@ -452,14 +464,23 @@ __device__ __forceinline__ void tile_step(const Tiles<C>& t, Rows<C>& w, const u
       }
   }
 
+}
+
+// O^T += V^T P^T of the tile in buffer `at`.
+template <class C>
+__device__ __forceinline__ void product(const Tiles<C>& t, Rows<C>& w, const Weights<C>& pf, int at) {
+  constexpr int ND = C::DT / 16, N = C::KT / 32 * ND, AHEAD = C::AHEAD, RING = AHEAD + 1;
+  typename Tiles<C>::Raw a[RING];
 #pragma unroll
-  for (int i = 0; i < KC * ND; ++i) {
-    const int kc = i / ND, db = i % ND, n = i + AHEAD;
-    if (n < KC * ND) a[n % RING] = t.v_frag(at, n / ND, n % ND);
+  for (int i = 0; i < AHEAD; ++i) a[i] = t.v_frag(at, i / ND, i % ND);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int n = i + AHEAD;
+    if (n < N) a[n % RING] = t.v_frag(at, n / ND, n % ND);
     const bf16x8 f = Tiles<C>::operand(a[i % RING]);
 #pragma unroll
     for (int cb = 0; cb < C::CB; ++cb)
-      w.o[db][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pf[kc][cb], w.o[db][cb], 0, 0, 0);
+      w.o[i % ND][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pf[i / ND][cb], w.o[i % ND][cb], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   }
 }
@@ -472,7 +493,7 @@ __device__ __forceinline__ void add_infinities(const Tiles<C>& t, Rows<C>& w, in
     const int64_t page = t.table[j >> t.p.page_shift];
     if (page < 0 || page >= t.p.num_pages) continue;
     const unsigned char* row =
-        t.p.v.base + page * t.p.v.page + t.head_v + (j & ((1 << t.p.page_shift) - 1)) * static_cast<int64_t>(t.p.v.token);
+        t.base_v + page * t.p.v.page + (j & ((1 << t.p.page_shift) - 1)) * static_cast<int64_t>(t.p.v.token);
 #pragma unroll
     for (int db = 0; db < C::DT / 16; ++db) {
       const int d = 16 * db + 4 * (t.lane >> 4);
@@ -683,10 +704,10 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
   const float c = p.c * k_scale;
   const auto in_part = [&](int32_t j0) { return j0 < inner.lo || j0 + C::KT > inner.hi; };
   u32x4 kr[C::KT / 16][C::KL];
-  const auto step = [&](const Tiles<C>& t, int at, int32_t j0, auto&& k_used) {
-    if (C::SHARED && (!busy || j0 >= any.hi || j0 + C::KT <= any.lo)) return;
-    tile_step(t, w, kr, at, j0, c, j0 < full.lo || j0 + C::KT > full.hi, k_used);
-  };
+  Scores<C> sc;
+  Weights<C> pf;
+  const auto sees = [&](int32_t j0) { return !C::SHARED || (busy && j0 < any.hi && j0 + C::KT > any.lo); };
+  const auto masked = [&](int32_t j0) { return j0 < full.lo || j0 + C::KT > full.hi; };
 
   if (threadIdx.x == 0) any_infinite = 0;
   __syncthreads();
@@ -694,18 +715,26 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
     Tiles<C> t(p, lds + (C::SHARED ? 0 : wave * 2 * C::BUF), lane, wave);
     t.open(b, head, m, j_begin);
     if constexpr (C::SHARED) {
-      t.request(j_begin, 0);
+      t.template request<false>(j_begin, 0);
+      t.template request<true>(j_begin, 0);
       for (int32_t i = 0; i < count; ++i) {
         const int32_t j0 = j_begin + i * C::KT;
         wait_loads<0>();   // this wavefront's rows of tile i are there,
         if (in_part(j0) && t.make_finite(i & 1)) any_infinite = 1;
         group_barrier();   // every wavefront's are, and all have read tile i - 1
-        if (i + 1 < count) t.request(j0 + C::KT, (i + 1) & 1);
-        step(t, i & 1, j0, [] {});
+        if (i + 1 < count) {
+          t.template request<false>(j0 + C::KT, (i + 1) & 1);
+          t.template request<true>(j0 + C::KT, (i + 1) & 1);
+        }
+        if (sees(j0)) {
+          scores(t, w, kr, i & 1, sc);
+          softmax(w, sc, pf, lane, j0, c, masked(j0));
+          product(t, w, pf, i & 1);
+        }
       }
     } else {
       if (wave < count) {
-        t.request(j_begin + wave * C::KT, 0);
+        t.template request<true>(j_begin + wave * C::KT, 0);
         t.request_k(j_begin + wave * C::KT, kr);
       }
       int at = 0;
@@ -713,16 +742,16 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
         const int32_t j0 = j_begin + i * C::KT, j1 = j0 + C::WAVES * C::KT;
         const bool more = i + C::WAVES < count;
         if (more) {
-          t.request(j1, at ^ 1);
+          t.template request<true>(j1, at ^ 1);
           wait_loads<C::V_LOADS>();  // all but those: this tile's
         } else {
           wait_loads<0>();
         }
         if (in_part(j0) && t.make_finite(at)) any_infinite = 1;
-        // the next K rows take the registers as soon as the scores are there
-        step(t, at, j0, [&] {
-          if (more) t.request_k(j1, kr);
-        });
+        scores(t, w, kr, at, sc);
+        if (more) t.request_k(j1, kr);  // the registers are free
+        softmax(w, sc, pf, lane, j0, c, masked(j0));
+        product(t, w, pf, at);
         asm volatile("" ::: "memory");  // the next request writes where this tile was read
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -820,7 +849,7 @@ Variant variant(const char* name) {
 
 // A kernel for sequences of up to `rows` rows, and one for more. dt: 64, 128 or 256.
 __attribute__((visibility("hidden"))) Variant few_rows(int dt, bool fp8, int rows);
-__attribute__((visibility("hidden"))) Variant many_rows(int dt, bool fp8);
+__attribute__((visibility("hidden"))) Variant many_rows(int dt, bool fp8, bool small);
 
 }  // namespace attn
 

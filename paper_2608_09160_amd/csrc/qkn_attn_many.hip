@@ -3,17 +3,20 @@
 
 namespace attn {
 
+// Much work: 128 rows to a workgroup, two wavefronts on a SIMD where the registers allow it. Little: 64 rows, for more
+// workgroups.
 template <int DT, bool FP8>
-using Many = Cfg<DT, FP8, 2, 4, true, 64, DT == 256 ? 1 : 2>;
+using Large = Cfg<DT, FP8, 2, 4, true, 64, DT == 256 ? 1 : 2>;
+template <int DT, bool FP8>
+using Small = Cfg<DT, FP8, 1, 4, true, 64, DT == 256 ? 1 : 2>;
 
-Variant many_rows(int dt, bool fp8) {
-  if (fp8)
-    return dt == 64 ? variant<Many<64, true>>("attn<64,128,shared>/fp8")
-                    : dt == 128 ? variant<Many<128, true>>("attn<128,128,shared>/fp8")
-                                : variant<Many<256, true>>("attn<256,128,shared>/fp8");
-  return dt == 64 ? variant<Many<64, false>>("attn<64,128,shared>/bf16")
-                  : dt == 128 ? variant<Many<128, false>>("attn<128,128,shared>/bf16")
-                              : variant<Many<256, false>>("attn<256,128,shared>/bf16");
+#define QKN_PICK(DT, FP8, F)                                             \
+  (small ? variant<Small<DT, FP8>>("attn<" #DT ",64,shared>/" F)        \
+         : variant<Large<DT, FP8>>("attn<" #DT ",128,shared>/" F))
+
+Variant many_rows(int dt, bool fp8, bool small) {
+  if (fp8) return dt == 64 ? QKN_PICK(64, true, "fp8") : dt == 128 ? QKN_PICK(128, true, "fp8") : QKN_PICK(256, true, "fp8");
+  return dt == 64 ? QKN_PICK(64, false, "bf16") : dt == 128 ? QKN_PICK(128, false, "bf16") : QKN_PICK(256, false, "bf16");
 }
 
 }  // namespace attn

@@ -59,12 +59,13 @@ def test_accepted(dry):
 
 @pytest.mark.parametrize("max_q,n_q,D,fp8,name", [
     (1, 8, 128, 0, "attn<128,16>/bf16"), (1, 32, 128, 0, "attn<128,16>/bf16"), (1, 34, 128, 0, "attn<128,32>/bf16"),
-    (5, 8, 128, 1, "attn<128,32>/fp8"), (16, 8, 128, 1, "attn<128,64>/fp8"), (17, 8, 128, 1, "attn<128,128,shared>/fp8"),
+    (5, 8, 128, 1, "attn<128,32>/fp8"), (16, 8, 128, 1, "attn<128,64>/fp8"), (17, 8, 128, 1, "attn<128,64,shared>/fp8"),
+    (4096, 8, 128, 0, "attn<128,128,shared>/bf16"),
     (1, 8, 64, 0, "attn<64,16>/bf16"), (1, 8, 8, 0, "attn<64,16>/bf16"), (1, 8, 72, 0, "attn<128,16>/bf16"),
-    (9, 8, 256, 0, "attn<256,128,shared>/bf16"), (0, 8, 256, 0, "attn<256,16>/bf16"),
+    (9, 8, 256, 0, "attn<256,64,shared>/bf16"), (0, 8, 256, 0, "attn<256,16>/bf16"),
 ])
 def test_kernel_choice(dry, max_q, n_q, D, fp8, name):
-    a = args(max_q=max_q, n_q=n_q, ldq=n_q * D, ldo=n_q * D)
+    a = args(max_q=max_q, n_q=n_q, ldq=n_q * D, ldo=n_q * D, T=max(64, max_q), max_kv=4096 + max_q)
     c = cache(head_dim=D, fp8=fp8, k_token=D, v_token=D, k_head=16 * D, v_head=16 * D, k_page=32 * D, v_page=32 * D)
     assert call(dry, a, c) == DRY
     assert L.qkn_last_launch()["kernel"] == name
@@ -72,7 +73,8 @@ def test_kernel_choice(dry, max_q, n_q, D, fp8, name):
 
 def test_workspace(dry):
     n = need(dry)
-    assert n > 0 and n % (64 * 8 * (4 * 128 + 8)) == 0
+    # a part of every workgroup that the chip holds (two a CU, 16 rows each), and where each row's parts are
+    assert n == 512 * 16 * (4 * 128 + 8) + 64 * 8 * 8
     assert call(dry, ws_bytes=n) == DRY
     assert call(dry, ws_bytes=n - 1) == L.QKN_EINVAL
     assert call(dry, ws=None) == L.QKN_EINVAL
