@@ -70,8 +70,9 @@ int64_t qkn_adapters_workspace_bytes(int64_t T, int64_t hidden, int rank, int ns
  * strides below the row width, a_adapter or b_adapter < 0; a workspace that is
  * NULL or too small.
  * QKN_ENOTSUP: hidden, d_local, rank, or a stride not a multiple of 8, a
- * tensor (the workspace) not 16-byte aligned; rank over 128; T over 2^24, or
- * hidden or d_local over 2^30.
+ * tensor (the workspace) not 16-byte aligned; rank over 128; T over 2^24,
+ * count over 2^24, hidden, d_local or ldb over 2^30, ldx over 2^20, lda over
+ * 2^26 or an adapter's stride over 2^38.
  * QKN_EOVERLAP: an output (y, partials, workspace) overlapping an input or
  * another output, in-place y apart.
  */
