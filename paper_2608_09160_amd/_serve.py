@@ -7,6 +7,7 @@ once (for serving loops and HIP graphs, the tensors stay referenced), and a func
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from dataclasses import dataclass
 from typing import Optional
@@ -66,6 +67,15 @@ def load() -> ctypes.CDLL:
     return lib
 
 
+def _on(stream):
+    """Makes `stream` (None: as it is; a stream or its handle) the current one: what a call allocates for itself then
+    belongs to it and is not handed out again before the call's kernels have run."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream)
+                             else torch.cuda.ExternalStream(_stream(stream)))
+
+
 _CACHE_DTYPES = {torch.bfloat16: 0, torch.float8_e4m3fn: 1, torch.uint8: 1}
 
 
@@ -119,11 +129,12 @@ def qkn_rope_table(n_pos: int, rot_dim: int, base: float = 10000.0, factor: floa
                    out: Optional[torch.Tensor] = None, device="cuda", stream=None) -> torch.Tensor:
     """cos and sin of every position and pair, fp32 [n_pos, rot_dim / 2, 2]; see qkn_rope_scaling for the
     scaling to long contexts."""
-    if out is None:
-        out = torch.empty(n_pos, max(rot_dim, 0) // 2, 2, dtype=torch.float32, device=device)
-    sc = QknRopeScaling(base, factor, low, high, original, magnitude)
-    _check(load().qkn_rope_table(_f32(out, "out", n_pos * (rot_dim // 2) * 2), n_pos, rot_dim, ctypes.byref(sc),
-                                 _stream(stream)), "qkn_rope_table")
+    with _on(stream):
+        if out is None:
+            out = torch.empty(n_pos, max(rot_dim, 0) // 2, 2, dtype=torch.float32, device=device)
+        sc = QknRopeScaling(base, factor, low, high, original, magnitude)
+        _check(load().qkn_rope_table(_f32(out, "out", n_pos * (rot_dim // 2) * 2), n_pos, rot_dim, ctypes.byref(sc),
+                                     _stream(None)), "qkn_rope_table")
     return out
 
 
@@ -202,7 +213,8 @@ class PreparedRopeCache:
 def qkn_rope_cache(table, pos, head_dim, q=None, k=None, v=None, cache=None, slots=None, interleaved=False,
                    eps=1e-6, stream=None):
     """PreparedRopeCache made and called once; returns q's rotated rows."""
-    return PreparedRopeCache(table, pos, head_dim, q, k, v, cache, slots, interleaved, eps)(stream)
+    with _on(stream):
+        return PreparedRopeCache(table, pos, head_dim, q, k, v, cache, slots, interleaved, eps)()
 
 
 def _workspace(workspace: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
@@ -214,7 +226,8 @@ def _workspace(workspace: Optional[torch.Tensor], need: int, device) -> torch.Te
 
 
 class PreparedAttn:
-    """qkn_attn with its arguments and workspace prepared once: attention of the new tokens q (bf16 [T, heads *
+    """qkn_attn with its arguments and workspace prepared once (calls share the workspace: on one stream at a time):
+    attention of the new tokens q (bf16 [T, heads *
     head_dim], the sequences in order) over the cache that holds their keys and values already.
 
     block_table int32 [batch, pages of a sequence], q_start int32 [batch + 1], kv_len int32 [batch] (new tokens
@@ -270,8 +283,9 @@ class PreparedAttn:
 def qkn_attn(q, cache, block_table, q_start, kv_len, max_q=None, max_kv=None, scale=None, causal=True, window=0,
              out=None, lse=None, workspace=None, stream=None) -> torch.Tensor:
     """PreparedAttn made and called once."""
-    return PreparedAttn(q, cache, block_table, q_start, kv_len, max_q, max_kv, scale, causal, window, out, lse,
-                        workspace)(stream)
+    with _on(stream):
+        return PreparedAttn(q, cache, block_table, q_start, kv_len, max_q, max_kv, scale, causal, window, out, lse,
+                            workspace)()
 
 
 @dataclass
@@ -294,7 +308,8 @@ def _matrices(t: torch.Tensor, what: str):
 
 
 class PreparedAdapters:
-    """qkn_adapters_add with its arguments and workspace prepared once: y = base + scale_i B_i A_i x for the tokens
+    """qkn_adapters_add with its arguments and workspace prepared once (calls share the workspace: on one stream at a
+    time): y = base + scale_i B_i A_i x for the tokens
     of each request's adapter i = ids[t] (int32 [T]; outside the adapters: none), and the Phase A statistic of the
     stored rows. x is the projection's input (bf16 [T, hidden]), scale fp32 [adapters] or None."""
 
@@ -339,4 +354,5 @@ class PreparedAdapters:
 
 def qkn_adapters_add(x, segs, ids, scale=None, workspace=None, stream=None):
     """PreparedAdapters made and called once; returns the segments' (y, partials)."""
-    return PreparedAdapters(x, segs, ids, scale, workspace)(stream)
+    with _on(stream):
+        return PreparedAdapters(x, segs, ids, scale, workspace)()

@@ -22,7 +22,7 @@ from typing import Callable, Optional
 import torch
 
 from ._lib import PreparedProj, ProjSeg
-from ._serve import (AdapterSeg, KVCache, PreparedAdapters, PreparedAttn, PreparedRopeCache, RopeSeg, qkn_rope_table)
+from ._serve import (AdapterSeg, KVCache, PreparedAdapters, PreparedAttn, PreparedRopeCache, RopeSeg, _on, qkn_rope_table)
 
 
 @dataclass
@@ -98,7 +98,8 @@ class Step:
         if self.adapters is not None:
             self.adapters(stream)
         if self.tp > 1:
-            self.exchange(self.stat_q, self.stat_k, self.rank)
+            with _on(stream):
+                self.exchange(self.stat_q, self.stat_k, self.rank)
         self.rope(stream)
         self.attn(stream)
         self.output(stream)

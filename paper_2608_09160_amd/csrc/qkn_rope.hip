@@ -8,7 +8,15 @@
 // apart by rot / 2, so that a unit holds whole pairs and no value crosses lanes; for neighbouring pairs and for
 // the elements that pass they follow each other. V = 8 is one 16-byte vector a group. A wavefront takes 64 units
 // of one token (its statistics, position and slot are then scalars), Q's heads first, then K's, then V's.
-// No loop: every wavefront asks for all its rows at once and ends.
+// No loop: every wavefront asks for all its rows at once and ends. (A loop over tokens that asks for the next one's rows
+// ahead and keeps gamma in registers: 35 to 48 us for the prompt below, by the number of wavefronts, and 139 to 181 us
+// for the FP8 one.)
+//
+// Measured: 8192 tokens of 16 + 4 + 4 heads of 128 with the norm, bf16 cache, 105 MB: 35.7 us, 2.9 TB/s; 32768 tokens of
+// 16 + 2 + 2 heads into an FP8 cache, 337 MB: 109 us, 3.1 TB/s, where a copy of as many bytes reaches 5 to 5.9. 42 % of the SIMDs' cycles are
+// vector instructions (bf16 in and out, norm, rotation, addresses); the rest is waiting: position -> table, slot -> cache,
+// statistic -> scale follow each other in a wavefront's life of 9 us, with 24 wavefronts on a CU. 64 tokens: 5.1 us, a
+// launch.
 
 #include <string.h>
 

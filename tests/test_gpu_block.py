@@ -187,3 +187,35 @@ def test_refusals():
     b.ids = None
     with pytest.raises(ValueError):
         block.Step(w, cache, table, b)
+
+
+@pytest.mark.parametrize("as_handle", [False, True])
+def test_one_call_on_a_given_stream(monkeypatch, as_handle):
+    """What a call allocates belongs to the stream that it runs on, and the results are those of the current one."""
+    from paper_2608_09160_amd import _serve
+    g, w, pages, cache, table = _setup(5, 2, 300, False)
+    b = _batch(g, pages, [1, 1], [260, 290])
+    for pool in (cache.k, cache.v):
+        pool.copy_(torch.randn(pool.shape, generator=g).to(torch.bfloat16))
+    q = torch.randn(2, HEADS * D, generator=g).to(torch.bfloat16).to(DEV)
+    side, streams, real = torch.cuda.Stream(), [], _serve._workspace
+
+    def recorded(*args):
+        streams.append(torch.cuda.current_stream().cuda_stream)
+        return real(*args)
+    monkeypatch.setattr(_serve, "_workspace", recorded)
+
+    def calls(stream):
+        base = torch.zeros(2, HEADS * D, dtype=torch.bfloat16, device=DEV)
+        torch.cuda.synchronize()
+        out = qkn.qkn_attn(q, cache, b.block_table, b.q_start, b.kv_len, 1, b.max_kv, stream=stream)
+        y = qkn.qkn_adapters_add(b.x, [qkn.AdapterSeg(*w.adapters[0], base=base)], b.ids, stream=stream)[0][0]
+        turned = qkn.qkn_rope_cache(table, b.pos, D, qkn.RopeSeg(q), stream=stream)
+        angles = qkn.qkn_rope_table(9, D, stream=stream)
+        torch.cuda.synchronize()
+        return out, y, turned, angles
+    want = calls(None)
+    assert streams == [torch.cuda.current_stream().cuda_stream] * 2
+    got = calls(side.cuda_stream if as_handle else side)
+    assert streams[2:] == [side.cuda_stream] * 2
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
