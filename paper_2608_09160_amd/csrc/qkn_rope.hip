@@ -8,15 +8,14 @@
 // apart by rot / 2, so that a unit holds whole pairs and no value crosses lanes; for neighbouring pairs and for
 // the elements that pass they follow each other. V = 8 is one 16-byte vector a group. A wavefront takes 64 units
 // of one token (its statistics, position and slot are then scalars), Q's heads first, then K's, then V's.
-// No loop: every wavefront asks for all its rows at once and ends. (A loop over tokens that asks for the next one's rows
-// ahead and keeps gamma in registers: 35 to 48 us for the prompt below, by the number of wavefronts, and 139 to 181 us
-// for the FP8 one.)
+// No loop: every wavefront asks for all its rows at once and ends. Its loads, scalars among them, all go out before the
+// first of them is waited for, on every lane alike (in branches by kind of row, with the slot read behind the stores, the
+// prompt below took 35.7 us and the FP8 one 109). A loop over tokens that asks for the next one's rows ahead and keeps
+// gamma in registers was no faster than that: 35 to 48 us, 139 to 181.
 //
-// Measured: 8192 tokens of 16 + 4 + 4 heads of 128 with the norm, bf16 cache, 105 MB: 35.7 us, 2.9 TB/s; 32768 tokens of
-// 16 + 2 + 2 heads into an FP8 cache, 337 MB: 109 us, 3.1 TB/s, where a copy of as many bytes reaches 5 to 5.9. 42 % of the SIMDs' cycles are
-// vector instructions (bf16 in and out, norm, rotation, addresses); the rest is waiting: position -> table, slot -> cache,
-// statistic -> scale follow each other in a wavefront's life of 9 us, with 24 wavefronts on a CU. 64 tokens: 5.1 us, a
-// launch.
+// Measured: 8192 tokens of 16 + 4 + 4 heads of 128 with the norm, bf16 cache, 105 MB: 24.6 us, 4.3 TB/s; 32768 tokens of
+// 16 + 2 + 2 heads into an FP8 cache, 337 MB: 71 us, 4.7 TB/s; a copy of as many bytes reaches 5 to 5.9. 64 tokens: 5.1 us, a
+// launch and one chain of latencies (position -> angles).
 
 #include <string.h>
 
@@ -64,17 +63,23 @@ struct RopeParams {
   FastDiv per_head, parts;     // units of a head; wavefronts of a token
 };
 
-// Sum over the ranks, ascending, as Phase B adds them. Four loads in flight at a time; the address is the same on
-// all lanes.
-__device__ __forceinline__ float rank_sum(const float* __restrict__ partials, int64_t t, int64_t T, int tp) {
-  float S = 0.0f;
-  for (int r = 0; r < tp; r += 4) {
-    float v[4];
+// A token's first statistics (past tp the last one's again). The address is the same on all lanes.
+constexpr int kRanks = 4;
+__device__ __forceinline__ void load_ranks(const float* __restrict__ partials, int64_t t, int64_t T, int tp, int r0,
+                                           float (&v)[kRanks]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = partials[(r + i < tp ? r + i : tp - 1) * T + t];
+  for (int i = 0; i < kRanks; ++i) v[i] = partials[(r0 + i < tp ? r0 + i : tp - 1) * T + t];
+}
+// Sum over the ranks, ascending, as Phase B adds them; `v`: the first ones, asked for before.
+__device__ __forceinline__ float rank_sum(const float* __restrict__ partials, int64_t t, int64_t T, int tp,
+                                          float (&v)[kRanks]) {
+  float S = v[0];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (r + i < tp) S = (r + i == 0) ? v[i] : S + v[i];
+  for (int i = 1; i < kRanks; ++i) S = i < tp ? S + v[i] : S;
+  for (int r = kRanks; r < tp; r += kRanks) {
+    load_ranks(partials, t, T, tp, r, v);
+#pragma unroll
+    for (int i = 0; i < kRanks; ++i) S = r + i < tp ? S + v[i] : S;
   }
   return S;
 }
@@ -121,10 +126,10 @@ __device__ __forceinline__ void store_fp8(uint8_t* p, const float (&f)[V], float
 // One unit of one token into the cache.
 template <int V, bool FP8>
 __device__ __forceinline__ void store_cache(const PoolDev& pool, int64_t page, int64_t row, int head, int a, int b,
-                                            bool has_b, const float (&fa)[V], const float (&fb)[V]) {
+                                            bool has_b, float scale, const float (&fa)[V], const float (&fb)[V]) {
   const int64_t at = page * pool.page + head * pool.head + row * pool.token;
   if constexpr (FP8) {
-    const float rcp = pool.scale ? 1.0f / pool.scale[head] : 1.0f;
+    const float rcp = 1.0f / scale;
     uint8_t* p = static_cast<uint8_t*>(pool.base) + at;
     store_fp8<V>(p + a, fa, rcp);
     if (has_b) store_fp8<V>(p + b, fb, rcp);
@@ -151,46 +156,54 @@ __global__ __launch_bounds__(64 * kWaves) void qkn_rope(const RopeParams p) {
   const bool apart = turns && !p.interleaved;  // a pair's elements are rot / 2 apart
   const int a = apart ? uh * V : 2 * uh * V;
   const int b = apart ? a + p.half : a + V;
-  const bool live = u < p.units, has_b = V > 1 || b < p.D;  // an odd head ends in half a unit
+  const bool has_b = V > 1 || b < p.D;  // an odd head ends in half a unit
+  if (u >= p.units) return;             // lanes share nothing from here on
 
-  float fa[V] = {}, fb[V] = {};
-  if (live) {
-    const uint16_t* x = (of_q ? p.q.x + t * p.q.ldx : of_v ? p.v + t * p.ldv : p.k.x + t * p.k.ldx) + head * p.D;
-    load_group<V>(x + a, fa);
-    if (has_b) load_group<V>(x + b, fb);
+  float fa[V], fb[V];
+  const uint16_t* x = (of_q ? p.q.x + t * p.q.ldx : of_v ? p.v + t * p.ldv : p.k.x + t * p.k.ldx) + head * p.D;
+  load_group<V>(x + a, fa);
+  load_group<V>(x + (has_b ? b : a), fb);
+
+  // What the wavefront has in common, and what every lane needs next: all of it asked for before any of it is used, by
+  // all lanes alike (V's units, which need no gamma and no angle, read the first ones), so that the waits are one.
+  int32_t at = 0;
+  int64_t slot = -1;
+  float scale = 1.0f;
+  float ranks_q[kRanks] = {}, ranks_k[kRanks] = {};
+  if (p.half) at = p.pos[t];
+  if (p.cached) {
+    slot = p.slots[t];
+    if constexpr (FP8) {
+      const float* sc = of_v ? p.vp.scale : p.kp.scale;
+      if (sc && !of_q) scale = sc[head];
+    }
   }
-
+  if (p.q.w) load_ranks(p.q.partials, t, p.T, p.tp, 0, ranks_q);
+  if (p.k.w) load_ranks(p.k.partials, t, p.T, p.tp, 0, ranks_k);
   const float* w = of_q ? p.q.w : of_v ? nullptr : p.k.w;
-  float wa[V], wb[V];
-  if (live && w) {
-    w += head * p.D;
+  float wa[V], wb[V], cs[V][2];
+  if (p.q.w || p.k.w) {
+    const float* any = p.q.w ? p.q.w : p.k.w;
+    const float* w1 = w ? w + head * p.D + a : any;
+    const float* w2 = w && has_b ? w + head * p.D + b : any;
 #pragma unroll
-    for (int e = 0; e < V; ++e) wa[e] = w[a + e];
+    for (int e = 0; e < V; ++e) wa[e] = w1[e];
 #pragma unroll
-    for (int e = 0; e < V; ++e) wb[e] = has_b ? w[b + e] : 0.0f;
+    for (int e = 0; e < V; ++e) wb[e] = w2[e];
   }
-
-  // position: pair i of this unit and the next ones
-  float cs[V][2];
-  bool inside = true;
-  if (p.half) {
-    int64_t at = p.pos[t];
-    inside = at >= 0 && at < p.n_pos;
-    if (live && turns) {
-      const float* row = p.table + 2 * ((inside ? at : 0) * p.half + uh * V);
-      const float nan = __builtin_nanf("");
+  const bool inside = at >= 0 && at < p.n_pos;  // or nothing turns
+  if (p.half && inside) {
+    const float* row = p.table + 2 * (static_cast<int64_t>(at) * p.half + (turns ? uh * V : 0));
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        cs[e][0] = inside ? row[2 * e] : nan;
-        cs[e][1] = inside ? row[2 * e + 1] : nan;
-      }
+    for (int e = 0; e < V; ++e) {
+      cs[e][0] = row[2 * e];
+      cs[e][1] = row[2 * e + 1];
     }
   }
 
   float inv_q = 1.0f, inv_k = 1.0f;
-  if (p.q.w) inv_q = __builtin_amdgcn_rsqf(__builtin_fmaf(rank_sum(p.q.partials, t, p.T, p.tp), p.q.rcp_d, p.eps));
-  if (p.k.w) inv_k = __builtin_amdgcn_rsqf(__builtin_fmaf(rank_sum(p.k.partials, t, p.T, p.tp), p.k.rcp_d, p.eps));
-  if (!live) return;
+  if (p.q.w) inv_q = __builtin_amdgcn_rsqf(__builtin_fmaf(rank_sum(p.q.partials, t, p.T, p.tp, ranks_q), p.q.rcp_d, p.eps));
+  if (p.k.w) inv_k = __builtin_amdgcn_rsqf(__builtin_fmaf(rank_sum(p.k.partials, t, p.T, p.tp, ranks_k), p.k.rcp_d, p.eps));
 
   if (w) {
     const float inv = of_q ? inv_q : inv_k;
@@ -200,7 +213,12 @@ __global__ __launch_bounds__(64 * kWaves) void qkn_rope(const RopeParams p) {
       fb[e] = fb[e] * wb[e] * inv;
     }
   }
-  if (turns) {
+  if (!inside) {
+    if (turns) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) fa[e] = fb[e] = __builtin_nanf("");
+    }
+  } else if (turns) {
     if (V > 1 && p.interleaved) {  // pairs (0, 1), (2, 3), ... of group a, then of group b
       if constexpr (V > 1) {
 #pragma unroll
@@ -230,11 +248,10 @@ __global__ __launch_bounds__(64 * kWaves) void qkn_rope(const RopeParams p) {
     if (has_b) store_bf16<V>(y + b, fb);
   }
   if (p.cached && !of_q) {
-    const int64_t slot = p.slots[t];
     if (slot >= 0 && slot < p.n_slots) {
       const int64_t page = slot >> p.page_shift, row = slot & p.page_mask;
-      if (of_v) store_cache<V, FP8>(p.vp, page, row, head, a, b, has_b, fa, fb);
-      else store_cache<V, FP8>(p.kp, page, row, head, a, b, has_b, fa, fb);
+      if (of_v) store_cache<V, FP8>(p.vp, page, row, head, a, b, has_b, scale, fa, fb);
+      else store_cache<V, FP8>(p.kp, page, row, head, a, b, has_b, scale, fa, fb);
     }
   }
 }
