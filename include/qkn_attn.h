@@ -14,7 +14,8 @@
  *         window > 0,
  *   out_i = sum_j exp(x_j) v_j / sum_j exp(x_j),   lse_i = log sum_j exp(x_j).
  * A token that sees no key (m < n leaves such tokens) has out = 0 and lse =
- * -infinity. Keys and values that a token does not see take no part, whatever
+ * -infinity, and so has a token of no sequence: q_start may begin above 0 and
+ * end below T, as in a replayed batch of fixed T with padding behind it. Keys and values that a token does not see take no part, whatever
  * they hold (a NaN in a later token's value reaches no earlier token).
  *
  * Arithmetic: products of bf16 values (an FP8 code is one exactly) summed in
@@ -41,10 +42,10 @@ extern "C" {
 
 /*
  *   q, out       bf16 [T, ldq], [T, ldo]: n_q * head_dim columns, heads in a
- *                row; T = q_start[batch] tokens of all sequences, in order.
+ *                row; the tokens of all sequences, in order, among T.
  *                out == q is not allowed.
  *   lse          fp32 [T, n_q], or NULL.
- *   q_start      int32 [batch + 1], ascending from 0 to T.
+ *   q_start      int32 [batch + 1], ascending, within 0 and T.
  *   kv_len       int32 [batch].
  *   block_table  int32 [batch, ld_table]: entry p of row b is the page that
  *                holds tokens [p * page_size, (p + 1) * page_size) of sequence
@@ -59,7 +60,8 @@ extern "C" {
  * What the device arrays hold cannot be checked before the launch; the
  * kernels stay inside the buffers whatever they hold: q_start is clamped to
  * [0, T], kv_len to [0, ld_table * page_size], and a page number outside
- * [0, num_pages) reads as zeros.
+ * [0, num_pages) reads as zeros. A q_start that is not ascending leaves what
+ * the tokens that it names twice or not at all receive undefined.
  */
 typedef struct qkn_attn_args {
   const uint16_t* q;

@@ -43,7 +43,8 @@ class Weights:
 @dataclass
 class Batch:
     """What a step runs on, all of it read on the device when the step runs: int32, slots int64. max_q and max_kv bound
-    the new and the cached tokens of a sequence for as long as the step is used."""
+    the new and the cached tokens of a sequence for as long as the step is used. Tokens behind the last sequence's (a
+    batch that has lost some: q_start 0, .., k, k, k, slots and ids -1) are padding, and zeros in the attention."""
 
     x: torch.Tensor            # bf16 [T, hidden]
     pos: torch.Tensor          # [T]

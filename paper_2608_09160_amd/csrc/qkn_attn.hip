@@ -15,6 +15,8 @@ using qkn_host::spans_overlap;
 // is a chain of latencies. GROUPS = 8, for few rows, which may have many parts: eight threads take every eighth part of
 // a row and are added through LDS (16 sequences of up to 32768 keys, 256 rows of up to 60 parts: 4.8 against 13.2 us).
 // GROUPS = 1, for many rows (12432 rows of 5 parts: 9.5 against 14.3 us).
+// parts_of has been written for every row, unless q_start is not ascending: then some rows have what the workspace held
+// before, so it is held against the launch before it is an index.
 constexpr int kJoinVecs = 32, kJoinThreads = 8 * kJoinVecs;
 template <int GROUPS>
 __global__ __launch_bounds__(kJoinThreads) void qkn_attn_join(const Params p, int32_t tile_rows) {
@@ -26,7 +28,8 @@ __global__ __launch_bounds__(kJoinThreads) void qkn_attn_join(const Params p, in
   const int d = (static_cast<int>(blockIdx.y) * kJoinVecs + vec) * 4;
   if (GROUPS == 1 && r >= p.T * p.n_q) return;
   const int32_t first = p.parts_of[r][0], v = p.parts_of[r][1], parts = v >> 8, i = v & 255;
-  if (parts <= 1) return;  // written already (GROUPS = 8: the whole workgroup's row)
+  const bool inside = (first < p.items * p.n_kv) & (int64_t{parts - 1} * p.n_kv <= first) & (i < tile_rows);
+  if (!(inside & (parts > 1))) return;  // parts <= 1: written already (GROUPS = 8: the whole workgroup's row)
   float top = neg_inf(), sum = 0.0f;
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
   constexpr int kBatch = GROUPS == 1 ? 8 : 4;  // parts whose loads go out together
@@ -128,12 +131,13 @@ Plan plan_of(const qkn_attn_args& a, const qkn_cache& c) {
     pl.v = many_rows(dt, c.fp8 != 0, pairs <= kSmallPairs);
   }
   pl.items = a.T * group / pl.v.rows + a.batch;  // the most row tiles that T tokens can make
+  if (pl.items < 1) pl.items = 1;                // no sequence: tokens to clear
   const int64_t slots = int64_t{pl.v.slots} * kCus / c.n_kv;
   // Split keys to fill the chip once, not more (two rounds of half the parts: 40.4 against 34.6 us for 64 single tokens
   // over up to 4096 keys), and not for less than a doubling (12 chunks of up to 512 tokens, window 1024: 41.7 split,
   // 29.7 us whole).
   const int64_t part = int64_t{kMinPart} * pl.v.step;
-  pl.split = 2 * pl.items <= slots && a.max_kv > part;
+  pl.split = a.batch && 2 * pl.items <= slots && a.max_kv > part;
   if (pl.split) {
     // the workgroups that take turns on the chip, or as many as the keys can use
     const int64_t most = pl.items * ((a.max_kv + part - 1) / part);
@@ -152,8 +156,9 @@ int attn_impl(const qkn_attn_args* args, const qkn_cache* cache, void* workspace
   if (rc != QKN_OK) return rc;
   const qkn_attn_args& a = *args;
   const qkn_cache& c = *cache;
-  if (a.T == 0 || a.batch == 0) return QKN_OK;
-  if (!a.q || !a.out || !a.q_start || !a.kv_len || (a.ld_table && !a.block_table) || (c.num_pages && (!c.k || !c.v)))
+  if (a.T == 0) return QKN_OK;
+  if (!a.q || !a.out || !a.q_start || (a.batch && (!a.kv_len || (a.ld_table && !a.block_table))) ||
+      (c.num_pages && (!c.k || !c.v)))
     return QKN_EINVAL;
   const Plan pl = plan_of(a, c);
   if (pl.ws_bytes && (!workspace || workspace_bytes < pl.ws_bytes)) return QKN_EINVAL;
@@ -250,7 +255,7 @@ extern "C" {
 int64_t qkn_attn_workspace_bytes(const qkn_attn_args* args, const qkn_cache* cache) {
   const int rc = attn::check_sizes(args, cache);
   if (rc != QKN_OK) return rc;
-  return args->T == 0 || args->batch == 0 ? 0 : attn::plan_of(*args, *cache).ws_bytes;
+  return args->T == 0 ? 0 : attn::plan_of(*args, *cache).ws_bytes;
 }
 
 int qkn_attn(const qkn_attn_args* args, const qkn_cache* cache, void* workspace, int64_t workspace_bytes,

@@ -80,7 +80,7 @@ struct Params {
   // split keys (NULL: not split): what each workgroup has of its row tile, and which workgroups have a row's parts
   float* part_o;                       // [workgroups, BM, D]
   f32x2* part_ml;                      // [workgroups, BM]: bound (log2 units) and sum; sum 0: nothing
-  int32_t (*parts_of)[2];              // [T * n_q]: workgroup of the first part; parts * 256 + row of the tile
+  int32_t (*parts_of)[2];              // [T * n_q]: workgroup of the first part; parts * 256 + row of the tile, or 0
   int32_t min_part;                    // key steps of a part, at least
 };
 
@@ -560,12 +560,13 @@ __device__ __forceinline__ Sequence sequence(const Params& p, int b) {
 struct Item {
   int32_t b, tile, part, parts, per;  // per: key steps of a part
   Sequence s;
+  int32_t first, end;                 // the first sequence's first token, the last one's end
 };
 
 // Deals the sequences' row tiles and parts to the p.items workgroups of a KV head. A part has `per` key steps, the
 // same for all sequences, the least with which the parts are no more than the workgroups: workgroups take equally
 // long whatever the sequences' lengths. Every wavefront finds the same from q_start and kv_len, a lane for a sequence.
-// False: nothing left for workgroup `idx`.
+// False: nothing left for workgroup `idx`; it.first and it.end are set all the same.
 template <class C>
 __device__ __forceinline__ bool schedule(const Params& p, int lane, int32_t idx, Item& it) {
   const int32_t G = static_cast<int32_t>(p.group.d);
@@ -584,6 +585,8 @@ __device__ __forceinline__ bool schedule(const Params& p, int lane, int32_t idx,
   };
   const auto parts = [](const Need& x, int32_t per) { return x.steps > per ? (x.steps + per - 1) / per : 1; };
   Need x = need(0);
+  it.first = __builtin_amdgcn_readlane(mine.q0, 0);
+  it.end = 0;
   int32_t per = 0x7fffffff, count = 0;  // not split
   if (p.part_o) {
     float work = 0.0f;
@@ -600,6 +603,8 @@ __device__ __forceinline__ bool schedule(const Params& p, int lane, int32_t idx,
     for (int base = 0; base < p.batch; base += 64) {
       if (base) x = need(base);
       count += last_lane(lane_sums(x.tiles * parts(x, per)));
+      const int32_t last = p.batch - 1 - base;
+      it.end = __builtin_amdgcn_readlane(mine.q0 + mine.n, last < 63 ? last : 63);
     }
     if (p.batch > 64) x = need(0);
     // with one part each the tiles of any ascending q_start are no more than the workgroups
@@ -631,6 +636,26 @@ __device__ __forceinline__ bool schedule(const Params& p, int lane, int32_t idx,
   return false;  // not reached
 }
 
+// The tokens that no sequence has, before the first one's and behind the last one's (the padding of a batch whose T is
+// fixed): zeros and a log-sum-exp of -infinity, as for a token that sees no key. The workgroups of a KV head take the
+// tokens in turn. Nothing to do is the rule, and costs no load: `schedule` has q_start. Where keys are split the rows
+// have no parts, which the joining reads for every row.
+__device__ __forceinline__ void clear_rest(const Params& p, int head, int32_t idx, int32_t first, int32_t end) {
+  if (end < first) end = first;
+  const int64_t G = p.group.d, rest = first + p.T - end;
+  for (int64_t i = idx; i < rest; i += p.items) {
+    const int64_t t = i < first ? i : end + (i - first);
+    uint16_t* row = p.out + t * p.ldo + head * G * p.D;
+    for (int64_t e = 8 * threadIdx.x; e < G * p.D; e += 8 * blockDim.x)
+      *reinterpret_cast<u32x4*>(row + e) = u32x4{0u, 0u, 0u, 0u};
+    for (int64_t h = threadIdx.x; h < G; h += blockDim.x) {
+      const int64_t r = t * p.n_q + head * G + h;
+      if (p.lse) p.lse[r] = neg_inf();
+      if (p.part_o) p.parts_of[r][0] = p.parts_of[r][1] = 0;
+    }
+  }
+}
+
 template <class C>
 __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const Params p) {
   __shared__ __align__(16) unsigned char lds[C::LDS];
@@ -643,7 +668,9 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
   const uint32_t bid = blockIdx.x, idx = div(bid, p.kv_heads);
   const int head = static_cast<int>(bid - idx * p.kv_heads.d);
   Item it;
-  if (!schedule<C>(p, lane, static_cast<int32_t>(idx), it)) return;
+  const bool any_left = schedule<C>(p, lane, static_cast<int32_t>(idx), it);
+  clear_rest(p, head, static_cast<int32_t>(idx), it.first, it.end);
+  if (!any_left) return;
   const int b = it.b;
   const int32_t q0 = it.s.q0, n = it.s.n, m = it.s.m, G = static_cast<int32_t>(p.group.d), R = n * G;
   const int32_t row0 = it.tile * C::BM;

@@ -263,3 +263,69 @@ def test_long(hq, hk, D, fp8, n, m):
             e = 2.0 ** -20 * (D ** -0.5 * np.abs(q[i]).max() * np.abs(k).max() * D + 20)
             O.check_rounded(_host(out)[i, h * D:(h + 1) * D], ref[0], (2.0 ** -8 + 2 * e) * size[0], "bf16", f"{i} {h}")
             assert abs(_host(lse)[i, h] - ref_lse[0]) <= e + 2.0 ** -22 * abs(ref_lse[0])
+
+
+def _padded_batch(which):
+    """(batch, q_start, tokens of a sequence): a batch among tokens that no sequence has, NaN in their rows of q."""
+    if which == "behind":  # a replayed batch of single tokens whose last sequences are gone
+        batch = Batch(20, [(1, 1500), (1, 20), (1, 800)] + [(0, 0)] * 5, 8, 2, 128)
+        start, T = [0, 1, 2, 3, 3, 3, 3, 3, 3], 8
+    elif which == "before and behind":
+        batch = Batch(21, [(1, 1300), (0, 40), (2, 900)], 8, 2, 128)
+        start, T = [5, 6, 6, 8], 70
+    elif which == "chunk":
+        batch = Batch(22, [(40, 900), (33, 33)], 8, 2, 128)
+        start, T = [3, 43, 76], 150
+    else:  # no sequence has a token
+        batch = Batch(23, [(0, 900), (0, 0)], 8, 2, 128)
+        start, T = [2, 2, 2], 9
+    q = torch.full((T, 8 * 128), float("nan"), dtype=torch.bfloat16)
+    q[start[0]:start[-1]] = batch.q
+    batch.q, batch.T = q, T
+    batch.q_start = torch.tensor(start, dtype=torch.int32)
+    return batch, range(start[0], start[-1])
+
+
+@pytest.mark.parametrize("fill", [0, 0x7F, 0xFF])
+@pytest.mark.parametrize("max_kv", [16, 1500])  # whole and split keys
+@pytest.mark.parametrize("which", ["behind", "before and behind", "chunk", "nothing"])
+def test_tokens_of_no_sequence_are_zeros(which, max_kv, fill):
+    """Whatever the workspace held before."""
+    batch, own = _padded_batch(which)
+    workspace = torch.full((1 << 26,), fill, dtype=torch.uint8, device=DEV)
+    out = torch.full((batch.T, 8 * 128), float("nan"), dtype=torch.bfloat16, device=DEV)
+    _, lse = batch.run(max_q=40 if which == "chunk" else 1, max_kv=max_kv, out=out, workspace=workspace)
+    batch.check(out, lse)
+    rest = [t for t in range(batch.T) if t not in own]
+    assert rest and out[rest].count_nonzero() == 0 and lse[rest].isneginf().all()
+
+
+@pytest.mark.parametrize("hq", [8, 80])
+def test_no_sequence_at_all(hq):
+    """T tokens and a batch of none."""
+    empty = torch.empty(0, dtype=torch.int32, device=DEV)
+    pool = torch.zeros(2, 2, 16, 64, dtype=torch.bfloat16, device=DEV)
+    q = torch.ones(5, hq * 64, dtype=torch.bfloat16, device=DEV)
+    lse = torch.ones(5, hq, device=DEV)
+    out = qkn.qkn_attn(q, qkn.KVCache(pool, pool.clone()), empty.view(0, 4), torch.zeros(1, dtype=torch.int32, device=DEV),
+                       empty, lse=lse)
+    assert out.count_nonzero() == 0 and lse.isneginf().all()
+
+
+@pytest.mark.parametrize("fill", [0, 0x7F, 0xFF])
+@pytest.mark.parametrize("start", [[0, 40, 20, 60], [60, 30, 10, 0], [0, 0, 1 << 30, 3], [50, 20, 60, -7]])
+def test_descending_starts_stay_inside_the_buffers(start, fill):
+    """Rows beside q, out and lse keep what they hold; the workspace's rest does too."""
+    batch = Batch(24, [(20, 900), (20, 700), (20, 1500)], 8, 2, 128)
+    batch.q_start = torch.tensor(start, dtype=torch.int32)
+    whole = torch.full((62, 1024), 3.0, dtype=torch.bfloat16, device=DEV)
+    sums = torch.full((62, 8), 3.0, device=DEV)
+    for max_q in (1, 20):
+        room = torch.full((1 << 26,), fill, dtype=torch.uint8, device=DEV)
+        call = qkn.PreparedAttn(batch.q.to(DEV), qkn.KVCache(batch._pool(batch.k), batch._pool(batch.v)),
+                                batch.table.to(DEV), batch.q_start.to(DEV), batch.kv_len.to(DEV), max_q=max_q, max_kv=1500,
+                                out=whole[1:61], lse=sums[1:61], workspace=room)
+        call()
+        torch.cuda.synchronize()
+        assert (whole[[0, 61]] == 3).all() and (sums[[0, 61]] == 3).all()
+        assert (room[1 << 25:] == fill).all()

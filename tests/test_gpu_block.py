@@ -219,3 +219,33 @@ def test_one_call_on_a_given_stream(monkeypatch, as_handle):
     got = calls(side.cuda_stream if as_handle else side)
     assert streams[2:] == [side.cuda_stream] * 2
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_replayed_graph_of_a_batch_that_loses_sequences():
+    """The step's shape stays, the sequences that are left come first: the live rows are those of the full batch, the
+    padding's are zeros, and nothing of the padding reaches the cache."""
+    prompts = [150, 3, 400, 90]
+    g, w, pages, cache, table = _setup(6, 4, 700, False)
+    block.Step(w, cache, table, _batch(g, pages, prompts, [0] * 4))()
+    b = _batch(g, pages, [1] * 4, prompts)
+    b.max_kv = 700  # enough to split keys; those of up to 512 stay whole, so that no result depends on the others' lengths
+    step = block.Step(w, cache, table, b)
+    assert step.attn.workspace.numel() > 16  # split keys
+    full = step().clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    pools = cache.k.clone(), cache.v.clone()
+    for live in (4, 2, 1, 3, 0, 4):
+        b.q_start.copy_(torch.arange(5).clamp(max=live).int())
+        b.kv_len.copy_(torch.tensor([(m + 1) * (i < live) for i, m in enumerate(prompts)], dtype=torch.int32))
+        b.slots.copy_(torch.where(torch.arange(4, device=DEV) < live,
+                                  pages.slots(torch.arange(4, device=DEV), b.pos), -1))
+        step.attn.workspace.fill_(0x7F)  # as if other calls had used it
+        step.out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert step.attn.out[live:].count_nonzero() == 0 and step.out[live:].count_nonzero() == 0
+        assert torch.equal(step.out[:live], full[:live])
+        assert torch.equal(cache.k, pools[0]) and torch.equal(cache.v, pools[1])
