@@ -87,7 +87,8 @@ typedef struct qkn_attn_args {
  * Bytes of device workspace qkn_attn needs for these arguments (the partial
  * results of split keys; 0 where they are not split); negative status for
  * sizes that qkn_attn refuses. Depends on T, batch, n_q, max_q, max_kv and the
- * cache's sizes only.
+ * cache's sizes only: one workspace serves layers of different windows and
+ * masks, one after the other.
  */
 int64_t qkn_attn_workspace_bytes(const qkn_attn_args* args, const qkn_cache* cache);
 

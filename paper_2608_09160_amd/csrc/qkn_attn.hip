@@ -116,20 +116,11 @@ int check_sizes(const qkn_attn_args* a, const qkn_cache* c) {
   return QKN_OK;
 }
 
-Plan plan_of(const qkn_attn_args& a, const qkn_cache& c) {
+// The workgroups of kernel v, and their workspace.
+Plan plan_with(const qkn_attn_args& a, const qkn_cache& c, const Variant& v) {
   Plan pl{};
-  const int dt = c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256;
-  const int64_t group = a.n_q / c.n_kv, rows = (a.max_q < 1 ? 1 : a.max_q) * group;
-  const bool few = rows <= (dt == 256 ? 32 : 64);
-  if (few) {
-    pl.v = few_rows(dt, c.fp8 != 0, static_cast<int>(rows));
-  } else {
-    // keys that a row sees, about, and pairs of 64 rows and 64 keys in all
-    int64_t keys = a.max_kv - (a.causal ? (a.max_q < a.max_kv ? a.max_q : a.max_kv) / 2 : 0);
-    if (a.window && a.window < keys) keys = a.window;
-    const int64_t pairs = (a.T * group + 63) / 64 * c.n_kv * ((keys + 63) / 64);
-    pl.v = many_rows(dt, c.fp8 != 0, pairs <= kSmallPairs);
-  }
+  pl.v = v;
+  const int64_t group = a.n_q / c.n_kv;
   pl.items = a.T * group / pl.v.rows + a.batch;  // the most row tiles that T tokens can make
   if (pl.items < 1) pl.items = 1;                // no sequence: tokens to clear
   const int64_t slots = int64_t{pl.v.slots} * kCus / c.n_kv;
@@ -148,6 +139,26 @@ Plan plan_of(const qkn_attn_args& a, const qkn_cache& c) {
   }
   pl.grid = pl.items * c.n_kv;
   return pl;
+}
+
+// The kernel, of two that may serve where rows are many: little work, or much.
+Plan plan_of(const qkn_attn_args& a, const qkn_cache& c, int64_t* workspace_bytes = nullptr) {
+  const int dt = c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256;
+  const int64_t group = a.n_q / c.n_kv, rows = (a.max_q < 1 ? 1 : a.max_q) * group;
+  const bool few = rows <= (dt == 256 ? 32 : 64);
+  if (few) {
+    const Plan pl = plan_with(a, c, few_rows(dt, c.fp8 != 0, static_cast<int>(rows)));
+    if (workspace_bytes) *workspace_bytes = pl.ws_bytes;
+    return pl;
+  }
+  // keys that a row sees, about, and pairs of 64 rows and 64 keys in all
+  int64_t keys = a.max_kv - (a.causal ? (a.max_q < a.max_kv ? a.max_q : a.max_kv) / 2 : 0);
+  if (a.window && a.window < keys) keys = a.window;
+  const int64_t pairs = (a.T * group + 63) / 64 * c.n_kv * ((keys + 63) / 64);
+  const Plan small = plan_with(a, c, many_rows(dt, c.fp8 != 0, true)), large = plan_with(a, c, many_rows(dt, c.fp8 != 0, false));
+  // the mask chooses between them, not the workspace: one serves a model's layers with and without a window
+  if (workspace_bytes) *workspace_bytes = small.ws_bytes > large.ws_bytes ? small.ws_bytes : large.ws_bytes;
+  return pairs <= kSmallPairs ? small : large;
 }
 
 int attn_impl(const qkn_attn_args* args, const qkn_cache* cache, void* workspace, int64_t workspace_bytes,
@@ -255,7 +266,10 @@ extern "C" {
 int64_t qkn_attn_workspace_bytes(const qkn_attn_args* args, const qkn_cache* cache) {
   const int rc = attn::check_sizes(args, cache);
   if (rc != QKN_OK) return rc;
-  return args->T == 0 ? 0 : attn::plan_of(*args, *cache).ws_bytes;
+  if (args->T == 0) return 0;
+  int64_t bytes = 0;
+  attn::plan_of(*args, *cache, &bytes);
+  return bytes;
 }
 
 int qkn_attn(const qkn_attn_args* args, const qkn_cache* cache, void* workspace, int64_t workspace_bytes,

@@ -149,3 +149,18 @@ def test_struct_layout_matches_header(tmp_path):
         name, value = line.split()
         want = ctypes.sizeof(S.QknAttnArgs) if name == "qkn_attn_args" else getattr(S.QknAttnArgs, name).offset
         assert int(value) == want, name
+
+
+@pytest.mark.parametrize("T,batch,n_q,D,max_q,max_kv", [
+    (1024, 1, 16, 128, 1024, 16384), (777, 1, 16, 128, 777, 12001), (300, 4, 16, 64, 200, 30000), (64, 64, 16, 128, 1, 4096),
+    (90, 3, 16, 256, 60, 9000),
+])
+def test_one_workspace_serves_every_window(dry, T, batch, n_q, D, max_q, max_kv):
+    """Layers of one model differ in window and mask: the size depends on neither, and is enough for all."""
+    c = cache(n_kv=4, head_dim=D, k_token=D, v_token=D, k_head=16 * D, v_head=16 * D, k_page=64 * D, v_page=64 * D)
+    sizes = dict(T=T, batch=batch, n_q=n_q, ldq=n_q * D, ldo=n_q * D, max_q=max_q, max_kv=max_kv)
+    layers = [dict(causal=1, window=w) for w in (0, 1, 128, 1024, 1 << 30)] + [dict(causal=0)]
+    bytes_of = {need(dry, args(**sizes, **layer), c) for layer in layers}
+    assert len(bytes_of) == 1
+    for layer in layers:
+        assert call(dry, args(**sizes, **layer), c, ws_bytes=bytes_of.copy().pop()) == DRY
