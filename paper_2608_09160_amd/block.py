@@ -72,7 +72,8 @@ class Step:
             raise ValueError("batch.ids: needed with adapters")
         x, T, D = batch.x, batch.x.shape[0], cache.k.shape[3]
         self.batch, self.tp, self.rank, self.exchange = batch, tp, rank, exchange
-        self.stat_q, self.stat_k = (torch.zeros(tp, T, dtype=torch.float32, device=x.device) for _ in range(2))
+        # nothing is written here: the step may run on another stream than the current one
+        self.stat_q, self.stat_k = (torch.empty(tp, T, dtype=torch.float32, device=x.device) for _ in range(2))
         qk = [ProjSeg(w.wq, partials=self.stat_q[rank]), ProjSeg(w.wk, partials=self.stat_k[rank])]
         v = [ProjSeg(w.wv)]
         self.projections = [PreparedProj(x, qk), PreparedProj(x, v)]
