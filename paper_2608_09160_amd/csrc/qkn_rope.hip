@@ -361,7 +361,7 @@ int rope_impl(const qkn_rope_seg* q, const qkn_rope_seg* k, const uint16_t* v, i
       r.add(pool_span(c, c.v, c.v_page, c.v_head, c.v_token), true);
       vec = vec && aligned(c.v, to) && c.v_page % 8 == 0 && c.v_head % 8 == 0 && c.v_token % 8 == 0;
     }
-    if (k && v && c.k == c.v) return QKN_EOVERLAP;
+    if (k && v && c.num_pages && c.k == c.v) return QKN_EOVERLAP;
   }
   const bool two_pools = cache && k && v;  // they may share an allocation, their rows in turn
   for (int a = 0; a < r.n; ++a)

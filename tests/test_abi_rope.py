@@ -146,3 +146,10 @@ def test_struct_layouts_match_header(tmp_path):
         cls, _, field = name.partition(".")
         want = getattr(classes[cls], field).offset if field else ctypes.sizeof(classes[cls])
         assert int(value) == want, name
+
+
+def test_empty_pools_are_not_an_overlap(dry):
+    """A cache without pages has no pool to overlap: both may be NULL, as empty tensors are, or one address."""
+    assert call(dry, cache=cache(num_pages=0, k=None, v=None)) == DRY
+    assert call(dry, cache=cache(num_pages=0, k=BASE + 1000 * MB, v=BASE + 1000 * MB)) == DRY
+    assert call(dry, cache=cache(num_pages=0, k=None, v=None, fp8=1), k=seg(300, 2, y=None)) == DRY
