@@ -380,6 +380,8 @@ __global__ __launch_bounds__(64 * WAVES) void qkn_adapters_b(const Params p) {
         for (int e = 0; e < 4; ++e) {
           const f32x4& v = y[2 * h + e / 2][mt];
           out[e] = pack_bf16x2(bf16_lo(base[mt][h][e]) + v[2 * (e % 2)], bf16_hi(base[mt][h][e]) + v[2 * (e % 2) + 1]);
+          // a row without an adapter as it is: + 0 would turn -0 into 0 and change a NaN's bits
+          if (!has_adapter(p, own[mt])) out[e] = base[mt][h][e];
         }
         if (16 * mt + i16 < n && d < s.d) {
           *reinterpret_cast<u32x4*>(s.y + (t0 + 16 * mt + i16) * s.ldy + d) = out;

@@ -158,3 +158,19 @@ def test_no_tokens():
     y, _ = qkn.qkn_adapters_add(torch.empty(0, 64, dtype=torch.bfloat16, device=DEV), [seg],
                                 torch.empty(0, dtype=torch.int32, device=DEV))[0]
     assert y.shape == (0, 64)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("T", [3, 200, 1100])
+def test_rows_without_an_adapter_keep_their_bits(T, in_place):
+    """Negative zeros and NaN payloads among them."""
+    g = torch.Generator().manual_seed(6)
+    bits = torch.randint(-2 ** 15, 2 ** 15, (T, 64), generator=g, dtype=torch.int16).to(DEV)
+    bits[:, :4] = torch.tensor([-0x8000, 0x7F81, -0x7F, 0], dtype=torch.int16, device=DEV)  # -0, NaN, NaN, 0
+    base = bits.view(torch.bfloat16)
+    y = base if in_place else torch.zeros_like(base)
+    ids = torch.where(torch.arange(T) % 3 == 1, torch.arange(T) % 2, -1).int().to(DEV)
+    a, b = _bf16(g, 2, 8, 128, scale=0.1), _bf16(g, 2, 64, 8, scale=0.3)
+    want = bits.clone()
+    qkn.qkn_adapters_add(_bf16(g, T, 128), [qkn.AdapterSeg(a=a, b=b, y=y, base=base)], ids)
+    assert torch.equal(y.view(torch.int16)[ids < 0], want[ids < 0])
