@@ -8,6 +8,7 @@ once (for serving loops and HIP graphs, the tensors stay referenced), and a func
 from __future__ import annotations
 
 import contextlib
+import copy
 import ctypes
 from dataclasses import dataclass
 from typing import Optional
@@ -196,7 +197,8 @@ class PreparedRopeCache:
             if slots is None:
                 raise ValueError("slots: needed with a cache")
             ps = _index(slots, "slots", torch.int64, T)
-        self.q, self.k, self.v, self.cache = q, k, v, cache
+        # as they are now: the tensors stay referenced whatever becomes of the caller's objects
+        self.q, self.k, self.v, self.cache = copy.copy(q), copy.copy(k), v, copy.copy(cache)
         self._keep = (table, pos, slots)
         self._cache = cache.struct() if cache is not None else None
         self._segs = segs
@@ -270,7 +272,7 @@ class PreparedAttn:
         if need < 0:
             _check(int(need), "qkn_attn_workspace_bytes")
         self.workspace = _workspace(workspace, need, q.device)
-        self.q, self.out, self.lse, self.cache = q, out, lse, cache
+        self.q, self.out, self.lse, self.cache = q, out, lse, copy.copy(cache)
         self._keep = (block_table, q_start, kv_len, a, c)
         self._args = (ctypes.byref(a), ctypes.byref(c), self.workspace.data_ptr(), self.workspace.numel())
         self._fn = lib.qkn_attn
@@ -341,7 +343,7 @@ class PreparedAdapters:
         if need < 0:
             _check(int(need), "qkn_adapters_workspace_bytes")
         self.workspace = _workspace(workspace, need, x.device)
-        self.segs = segs
+        self.segs = [copy.copy(s) for s in segs]
         self._keep = (x, ids, scale)
         self._args = (px, ldx, T, hidden, arr, len(segs), rank, count, _index(ids, "ids", torch.int32, T),
                       _f32(scale, "scale", count), self.workspace.data_ptr(), self.workspace.numel())

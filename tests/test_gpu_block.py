@@ -249,3 +249,38 @@ def test_replayed_graph_of_a_batch_that_loses_sequences():
         assert step.attn.out[live:].count_nonzero() == 0 and step.out[live:].count_nonzero() == 0
         assert torch.equal(step.out[:live], full[:live])
         assert torch.equal(cache.k, pools[0]) and torch.equal(cache.v, pools[1])
+
+
+def test_prepared_calls_keep_their_tensors():
+    """A prepared call holds the addresses of its tensors: they live as long as it does, whatever becomes of the objects
+    that named them."""
+    import gc
+    import weakref
+    g, w, pages, cache, table = _setup(7, 2, 64, True)
+    b = _batch(g, pages, [1, 1], [20, 30])
+
+    def rows(width=HEADS * D, dtype=torch.bfloat16):
+        return torch.zeros(2, width, dtype=dtype, device=DEV)
+    q, k = (qkn.RopeSeg(rows(n), torch.ones(n, device=DEV), torch.ones(1, 2, device=DEV), n, rows(n))
+            for n in (HEADS * D, KV * D))
+    pools = qkn.KVCache(cache.k.clone(), cache.v.clone(), cache.k_scale.clone(), cache.v_scale.clone())
+    seg = qkn.AdapterSeg(w.adapters[0][0].clone(), w.adapters[0][1].clone(), rows(), torch.ones(2, device=DEV), rows())
+    calls = [qkn.PreparedRopeCache(table, b.pos, D, q, k, rows(KV * D), pools, b.slots),
+             qkn.PreparedAttn(rows(), pools, b.block_table, b.q_start, b.kv_len, 1, 64, lse=rows(HEADS, torch.float32)),
+             qkn.PreparedAdapters(rows(HIDDEN), [seg], b.ids.clone())]
+    refs = [weakref.ref(t) for holder in (q, k, pools, seg) for t in vars(holder).values() if torch.is_tensor(t)]
+    assert len(refs) == 4 + 4 + 4 + 5
+    for holder in (q, k, pools, seg):
+        for name, t in vars(holder).items():
+            if torch.is_tensor(t):
+                setattr(holder, name, None)
+    del t
+    gc.collect()
+    assert all(r() is not None for r in refs)
+    for call in calls:
+        call()
+    torch.cuda.synchronize()
+    calls.clear()
+    del call
+    gc.collect()
+    assert all(r() is None for r in refs)
