@@ -31,8 +31,9 @@ extern "C" {
  *   page_size   tokens of a page: a power of two, 1 to 65536.
  *   n_kv        KV heads of this rank (>= 1).
  *   head_dim    D (>= 1).
- *   strides     in elements; each at least head_dim. Pages of a pool must not
- *               share elements, nor may the two pools.
+ *   strides     in elements; each at least head_dim and at most 2^40, and from
+ *               a pool's first element to its last at most 2^46. Pages of a
+ *               pool must not share elements, nor may the two pools.
  */
 typedef struct qkn_cache {
   void* k;

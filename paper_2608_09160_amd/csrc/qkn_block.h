@@ -69,21 +69,29 @@ inline int log2_of(int64_t v) {
   return s;
 }
 
+// Elements from the first to the last of a pool.
+inline __int128 pool_extent(const qkn_cache& c, int64_t page, int64_t head, int64_t token) {
+  if (!c.num_pages) return 0;
+  return static_cast<__int128>(c.num_pages - 1) * page + static_cast<__int128>(c.n_kv - 1) * head +
+         static_cast<__int128>(c.page_size - 1) * token + c.head_dim;
+}
+
 // Sizes and strides of a cache; its pointers are checked where they are used.
 inline bool cache_ok(const qkn_cache& c) {
   if (c.num_pages < 0 || c.num_pages > (int64_t{1} << 31) || c.page_size < 1 || c.page_size > 65536 ||
       (c.page_size & (c.page_size - 1)) || c.n_kv < 1 || c.head_dim < 1)
     return false;
-  const int64_t most = int64_t{1} << 40;  // products of the strides below stay in 64 bits
+  const int64_t most = int64_t{1} << 40, space = int64_t{1} << 46;  // no pool is larger: offsets in it stay in 64 bits
   for (int64_t s : {c.k_page, c.k_head, c.k_token, c.v_page, c.v_head, c.v_token})
     if (s < c.head_dim || s > most) return false;
+  if (pool_extent(c, c.k_page, c.k_head, c.k_token) > space || pool_extent(c, c.v_page, c.v_head, c.v_token) > space)
+    return false;
   return c.fp8 || (!c.k_scale && !c.v_scale);
 }
 
 // Extent of a pool as one byte region (its gaps included).
 inline qkn_host::Span pool_span(const qkn_cache& c, const void* base, int64_t page, int64_t head, int64_t token) {
-  const int64_t n = c.num_pages ? (c.num_pages - 1) * page + (c.n_kv - 1) * head + (c.page_size - 1) * token + c.head_dim
-                                : 0;
+  const int64_t n = static_cast<int64_t>(pool_extent(c, page, head, token));
   return qkn_host::Span{reinterpret_cast<uintptr_t>(base), n ? 1 : 0, n, n, c.fp8 ? 1 : 2};
 }
 inline qkn_host::Span array_span(const void* p, int64_t n, int64_t esz) {

@@ -164,3 +164,14 @@ def test_one_workspace_serves_every_window(dry, T, batch, n_q, D, max_q, max_kv)
     assert len(bytes_of) == 1
     for layer in layers:
         assert call(dry, args(**sizes, **layer), c, ws_bytes=bytes_of.copy().pop()) == DRY
+
+
+def test_pools_beyond_the_address_space(dry):
+    """Page strides whose extent no address space has: the extent is the overlap test's, and must not wrap around."""
+    wide = dict(k_page=1 << 40, v_page=1 << 40)
+    assert call(dry, c=cache(num_pages=(1 << 24) + 1, **wide)) == L.QKN_EINVAL
+    assert call(dry, c=cache(num_pages=1 << 31, k_page=1 << 40)) == L.QKN_EINVAL
+    assert call(dry, c=cache(num_pages=1 << 31, v_page=1 << 40)) == L.QKN_EINVAL
+    assert call(dry, c=cache(num_pages=1, **wide)) == DRY  # the stride of one page is not used
+    far = cache(num_pages=33, k_page=1 << 28, v_page=1 << 28, v=BASE + (1 << 40))  # 16 GiB of k, read up to its last page
+    assert call(dry, args(out=BASE + 1000 * MB + (1 << 33)), far) == L.QKN_EOVERLAP
