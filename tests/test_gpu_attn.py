@@ -329,3 +329,61 @@ def test_descending_starts_stay_inside_the_buffers(start, fill):
         torch.cuda.synchronize()
         assert (whole[[0, 61]] == 3).all() and (sums[[0, 61]] == 3).all()
         assert (room[1 << 25:] == fill).all()
+
+
+@pytest.mark.parametrize("hq,window", [(4, 0), (40, 0), (2, 20), (40, 20), (130, 20)])
+@pytest.mark.parametrize("fp8,value", [(False, "nan"), (False, "inf"), (False, "-inf"), (True, "nan")])  # no infinity in e4m3fn
+def test_infinities_and_nan_of_a_key_are_in_the_rows_that_see_it(fp8, hq, window, value):
+    """A NaN, or a score of +infinity, makes the row NaN; a score of -infinity is a weight of 0."""
+    n, m = 37, 150
+    for j in (m - n - 3, m - n + 4, m - 20, m - 1):
+        bad = Batch(25, [(n, m), (1, 64)], hq, 1, 64, 16, fp8)
+        bad.k[int(bad.table[0, j // 16]), 0, j % 16, 9] = float(value)
+        out, lse = (_host(t) for t in bad.run(window=window))
+        largest = np.abs(_host(bad.k)[np.isfinite(_host(bad.k))]).max()
+        for b, (new, kept) in enumerate(bad.lens):
+            for h in range(hq):
+                q, k, v = bad.sequence(b, h)
+                ref, ref_lse = O.attention(q, k, v, 0.125, window=window)
+                size, _ = O.attention(q, k, np.abs(v), 0.125, window=window)
+                e = 2.0 ** -20 * (0.125 * np.abs(q).max() * largest * 2.0 * 64 + np.log2(kept + 2) + 4)  # scales: up to 1.5
+                rows = slice(n * b, n * b + new)
+                O.check_rounded(out[rows, 64 * h:64 * h + 64], ref, (2.0 ** -8 + 2 * e) * size, "bf16", f"{j} {b} {h}")
+                assert np.array_equal(np.isnan(lse[rows, h]), np.isnan(ref_lse))
+                ok = np.isfinite(ref_lse)
+                assert np.all(np.abs(lse[rows, h][ok] - ref_lse[ok]) <= e + 2.0 ** -22 * np.abs(ref_lse[ok]))
+                if b == 0:
+                    at = np.arange(m - n, m)
+                    sees = (at >= j) & ((at < j + window) if window else True)
+                    hit = sees if value == "nan" else sees & (q[:, 9] * float(value) == np.inf)
+                    assert np.array_equal(np.isnan(ref_lse), hit)  # the reference says so too
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("window", [1, 100, 700, 3000])
+@pytest.mark.parametrize("hq,hk", [(2, 2), (16, 1), (48, 1)])
+def test_windows_of_single_tokens_with_split_keys(window, hq, hk, fp8):
+    """Few rows, more keys than one part of them has: parts begin where the window does."""
+    batch = Batch(26, [(1, 2000), (1, 30), (0, 0), (1, 5000), (1, 1)], hq, hk, 128, 64, fp8)
+    batch.check(*batch.run(window=window), window=window)
+
+
+@pytest.mark.parametrize("window", [0, 300])
+@pytest.mark.parametrize("value", ["nan", "inf"])
+def test_infinities_and_nan_in_split_keys(value, window):
+    batch = Batch(27, [(1, 2100), (3, 1900)], 4, 1, 64)
+    for b, j in ((0, 5), (0, 2098), (1, 1896), (1, 1899)):
+        batch.v[int(batch.table[b, j // 16]), 0, j % 16, 40] = float(value)
+    clean = Batch(27, [(1, 2100), (3, 1900)], 4, 1, 64)
+    (out, lse), (want, want_lse) = batch.run(window=window), clean.run(window=window)
+    assert torch.equal(lse, want_lse)
+    out, want = out.view(4, 4, 64), want.view(4, 4, 64)
+    same = out == want
+    same[..., 40] = True
+    assert same.all()
+    hit = out[..., 40].isnan() if value == "nan" else out[..., 40] == float("inf")
+    # tokens at 2099 of the first sequence; 1897, 1898, 1899 of the second: 1899 is seen by the last one alone
+    assert hit.all()
+    batch.v[int(batch.table[1, 1896 // 16]), 0, 1896 % 16, 40] = 0.0
+    out = batch.run(window=window)[0].view(4, 4, 64)
+    assert out[1:3, :, 40].isfinite().all() and not out[3, :, 40].isfinite().any()
