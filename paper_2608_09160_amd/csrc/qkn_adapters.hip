@@ -533,8 +533,12 @@ int adapters_impl(const uint16_t* x, int64_t ldx, int64_t T, int64_t hidden, con
     p.seg[i] = SegDev{s.a,  s.b,     s.base, s.y,      s.partials, s.a_adapter,
                       s.lda, s.b_adapter, s.ldb, s.ldbase, s.ldy,      static_cast<int32_t>(s.d_local)};
   }
-  // tokens of a workgroup of the second launch: one while that fills the chip, for it reads B once for them all
-  p.nt = T <= 128 ? 1 : T <= 1024 ? 4 : 16;
+  // tokens of a workgroup of the second launch, which reads B once for them all: one while workgroups are few (hidden
+  // 4096, 2048 + 512 columns, both launches, us with 1 and with 4 tokens: 32 adapters of rank 16, 64 tokens 14.7 and 21.7,
+  // 160 17.0 and 23.6, 256 17.6 and 24.3, 384 23.1 and 26.4; runs of 8 of rank 64, 256 31.9 and 37.3, 384 45.2 and 43.3, 512
+  // 52.4 and 46.8, 768 53.3 and 36.5), then four, sixteen from where those are many (4 and 16 tokens: 768 36.5 and 37.6,
+  // 1024 38.5 and 38.1, 1536 44.3 and 39.5, 4096 87.1 and 60.9)
+  p.nt = T <= 256 ? 1 : T <= 1024 ? 4 : 16;
   const int nb = p.n <= 32 ? 2 : p.n <= 64 ? 4 : 8;
   const char* name = pl.gather ? "adapters<gather>" : "adapters<tiles>";
   const int lds = nb == 2 ? lds_a<2>() : nb == 4 ? lds_a<4>() : lds_a<8>();
