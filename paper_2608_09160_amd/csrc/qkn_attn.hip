@@ -14,7 +14,9 @@ using qkn_host::spans_overlap;
 // A row's parts, added in a fixed order: four elements a thread, 128 elements of 8 / GROUPS rows a workgroup. The launch
 // is a chain of latencies. GROUPS = 8, for few rows, which may have many parts: eight threads take every eighth part of
 // a row and are added through LDS (16 sequences of up to 32768 keys, 256 rows of up to 60 parts: 4.8 against 13.2 us).
-// GROUPS = 1, for many rows (12432 rows of 5 parts: 9.5 against 14.3 us).
+// GROUPS = 1, for many rows (12432 rows of 5 parts: 9.5 against 14.3 us). In between, whole calls with 8 and with 1, us: 64
+// tokens of 16 heads behind 29936 keys, 1024 rows, 34.0 and 36.9; 128 behind 15872, 2048 rows, 34.8 and 37.2; 48 single
+// tokens of 48 heads over 3000 keys, 2304 rows, 29.2 and 28.4; 256 behind 11744, 4096 rows, 46.3 and 44.7.
 // parts_of has been written for every row, unless q_start is not ascending: then some rows have what the workspace held
 // before, so it is held against the launch before it is an index.
 constexpr int kJoinVecs = 32, kJoinThreads = 8 * kJoinVecs;
@@ -81,7 +83,7 @@ __global__ __launch_bounds__(kJoinThreads) void qkn_attn_join(const Params p, in
   if (d == 0 && p.lse) p.lse[r] = sum == 0.0f ? neg_inf() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-constexpr int64_t kJoinFew = 4096;  // rows
+constexpr int64_t kJoinFew = 2048;  // rows
 // Key steps of a part, at least (few rows: 128 keys each, many: 64): a part costs a workgroup's start and a share of the
 // join (4 single tokens over up to 500 keys, D 128: 9.4 us whole, 11.6 in parts of two steps).
 constexpr int kMinPart = 4;
