@@ -17,9 +17,11 @@
  *
  * Arithmetic: A x of bf16 values summed in fp32; the products with B take the
  * fp32 value of scale * (A x), as the sum of three bf16 values, summed in
- * fp32; base added in fp32; one rounding. A request's result does
- * not depend on the other requests' values. Deterministic for given sizes and
- * ids: no atomics, fixed orders.
+ * fp32; base added in fp32; one rounding. An infinite element of B makes NaN
+ * of the values that it is part of (it meets the three in turn, which may be 0
+ * or of either sign). A row without an adapter keeps base's bits. A request's
+ * result does not depend on the other requests' values. Deterministic for
+ * given sizes and ids: no atomics, fixed orders.
  *
  * Conventions are those of qkn.h.
  */
@@ -71,8 +73,8 @@ int64_t qkn_adapters_workspace_bytes(int64_t T, int64_t hidden, int rank, int ns
  * NULL or too small.
  * QKN_ENOTSUP: hidden, d_local, rank, or a stride not a multiple of 8, a
  * tensor (the workspace) not 16-byte aligned; rank over 128; T over 2^24,
- * count over 2^24, hidden, d_local or ldb over 2^30, ldx over 2^20, lda over
- * 2^26 or an adapter's stride over 2^38.
+ * count over 2^24, hidden, d_local or ldb over 2^30, ldx of 2^21 or lda of
+ * 2^27 or more, or an adapter's stride over 2^38.
  * QKN_EOVERLAP: an output (y, partials, workspace) overlapping an input or
  * another output, in-place y apart.
  */

@@ -7,8 +7,12 @@
 // l mod 16, k 8 (l / 16) .. + 7; result column l mod 16, rows 4 (l / 16) .. + 3). A product's rows belong to one adapter:
 // tokens are listed by adapter first, x is read through the list. Bytes bound both launches (x, base and y, and in
 // decode the adapters): 64 tokens of 32 adapters of rank 16 (hidden 4096, 1024 + 256 columns, 10.6 MB) 11.8 us; 8192
-// tokens in runs of 8 adapters of rank 64 (2048 + 512 columns, 162 MB) 89 us, 43 of them the first launch, whose LDS
-// receives 201 MB, x once and A's rows once for 64 tokens.
+// tokens in runs of 8 adapters of rank 64 (2048 + 512 columns, 162 MB) 90 us, 43 of them the first launch, whose LDS
+// receives 201 MB, x once and A's rows once for 64 tokens, and which writes 34 MB of A x in 8 parts of hidden; the second
+// reads those, base and, once for 16 tokens, B: 300 MB with what the caches give twice, by its counters.
+// Above 512 tokens a product's tokens are of 64 consecutive ones, whose adapters take turns: made for prompts in runs. Ids
+// that change from token to token cost more there (hidden 4096, 1024 + 256 columns, rank 16, us in runs and mixed: 512
+// tokens of 64 adapters 23.6 and 22.7, 1024 of 8 16.4 and 31.0, of 64 27.7 and 106, 4096 of 64 27.2 and 137).
 
 #include <string.h>
 
@@ -266,7 +270,9 @@ __global__ __launch_bounds__(kThreads) void qkn_adapters_a(const Params p) {
 // us; 32 tokens 89.3, four wavefronts 97.3, sixteen 93.4): B comes from the caches, 16 tokens' base and y from memory.
 template <int WAVES, int RS>
 __global__ __launch_bounds__(64 * WAVES) void qkn_adapters_b(const Params p) {
-  constexpr int MT = 1, kTok = 16 * MT, kRow = 32 * RS + 8;  // rows of 16 bytes more: their reads start on other banks
+  // rows of 16 bytes more than 64 RS, a multiple of all banks' width from RS 4 on: conflicts are left (4.5e5 of 1.1e6 cycles
+  // of LDS reads at 8192 tokens of rank 64), about 2 % of the launch
+  constexpr int MT = 1, kTok = 16 * MT, kRow = 32 * RS + 8;
   __shared__ __align__(16) uint16_t parts[kParts][kTok][kRow];
   __shared__ float sums[WAVES][kTok];
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63;
@@ -420,8 +426,9 @@ Plan plan_of(int64_t T, int64_t hidden) {
   Plan pl{};
   pl.gather = T <= kGather;
   pl.tiles = pl.gather ? T : (T + kList - 1) / kList;
-  // few tokens: about 2048 workgroups, most of which find that they are not their adapter's first; else about four a
-  // CU (8192 tokens, hidden 4096, rank 64: 43 us, 47 with two, 83 with one)
+  // few tokens: about 2048 workgroups, most of which find that they are not their adapter's first (hidden 4096, 1024 + 256
+  // columns, us with 1024, 2048 and 4096: 64 tokens 11.8, 12.5 and 11.7; 128 of rank 64 21.4, 24.7 and 24.7; 256 20.9, 18.2 and
+  // 19.8; 512 of rank 64 59.4, 45.8 and 48.5); else about four a CU (8192 tokens, rank 64: 43 us, 47 with two, 83 with one)
   int64_t ks = pl.gather ? 2048 / (T < 1 ? 1 : T) : 4 * kCus / pl.tiles;
   const int64_t most = (hidden + 255) / 256 < 16 ? (hidden + 255) / 256 : 16;
   if (ks > most) ks = most;

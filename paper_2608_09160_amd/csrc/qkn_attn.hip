@@ -90,8 +90,11 @@ constexpr int kMinPart = 4;
 // Pairs of 64 rows and 64 keys up to which many-row launches take 64 rows to a workgroup (16 + 4 heads of 128, us with 64
 // and with 128 rows: prompts of 256 tokens 9.6 and 12.2, 1024 21.7 and 26.6, 2048 39.1 and 49.7, 8192 344 and 277; 128
 // tokens behind 8064 24.9 and 26.7, 512 behind 7680 54.1 and 49.9; 16 + 2 heads of 64, 12 chunks of up to 512 tokens,
-// window 1024, 26.0 and 29.6). They need more LDS reads for the same products, but
-// make more workgroups.
+// window 1024, 26.0 and 29.6; FP8 heads of 128: 2048 44.1 and 57.1, 4096 102 and 111, 8192 339 and 315, 512 behind 7680 64.1
+// and 55.6; FP8 heads of 64: 2048 31.5 and 40.9, 4096 69.8 and 77.9, 8192 215 and 195; heads of 256: 2048 73.0 and 85.9, 4096
+// 248 and 179, 128 behind 8064 44.8 and 41.6, 512 behind 7680 221 and 95.5). They read more from LDS for the same products, but
+// make more workgroups. No count of pairs suits all: FP8 prompts of 4096 tokens lose a tenth, heads of 256 with 128 tokens
+// behind 8064 the same.
 constexpr int64_t kSmallPairs = 12288;
 
 struct Plan {

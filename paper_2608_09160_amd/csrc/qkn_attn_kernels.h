@@ -28,14 +28,19 @@
 //           and a row is an operand as it is: they go to registers, LDS has V only, and with half the LDS a CU holds
 //           twice the wavefronts, so twice the bytes are on their way.
 // Over workgroups the keys are split further where rows alone do not fill the chip (`schedule`); qkn_attn_join adds the
-// parts in ascending order.
+// parts in a fixed order.
 //
-// What bounds it. Few rows: the cache's bytes. 64 single tokens over up to 4096 keys of 8 + 2 heads of 128, 139 MB, 33.9 us,
-// 4.1 TB/s (29.5 the products, 4.8 the join); 16 over up to 32768 FP8 keys of 16 + 2 heads, 158 MB, 39.6 us, 4.0 TB/s; 4
-// over up to 500 keys 9.5 us, latencies. Many rows: instruction issue. For 64 rows x 64 keys of 128 a SIMD issues 64 products (17.5
-// cycles each in the matrix core, 8 of issue), and around them the softmax's fma, exp (9 to 10 cycles a wavefront) and
-// conversions, about 2560 cycles in all, while the CU's LDS reads take 3072 for 8 wavefronts of 32 rows (the transposing
-// reads run at half rate). A prompt of 8192 tokens of 16 + 4 heads, 275 Gflop, takes 276 us, 1.0 Pflop/s: the two overlap in part only.
+// What bounds it (times of calls in a row; the first ones after a pause take up to a sixth longer). Few rows: the cache's bytes.
+// 64 single tokens over up to 4096 keys of 8 + 2 heads of 128, 139 MB, 34.3 us, 4.1 TB/s (4.7 the join);
+// 16 over up to 32768 FP8 keys of 16 + 2 heads, 158 MB, 39.7 us, 4.0 TB/s; 4 over up to 500 keys 9.7 us, latencies. Many rows:
+// instruction issue. A prompt of 8192 tokens of 16 + 4 heads, 275 Gflop, takes 274 to 286 us, 1.0 Pflop/s. By its counters
+// a SIMD's matrix core is busy for 264 k of the 523 k cycles (128 products of 16 cycles for 64 rows x 64 keys of 128), and
+// the 372 other vector instructions of such a block (the softmax's fma, exp and conversions, most of them) are issued for
+// 1800 cycles, 227 k in all: products and softmax take turns more than they overlap. The LDS is no bound: its reads, 4
+// cycles for 16 bytes a lane and 2 for a transposing one of 8, take 133 k. Windowed chunks (12 of up to 512 tokens, window
+// 1024, 16 + 2 heads of 64, 25.8 us) too: a wavefront's 16 rows and 64 keys take 256 cycles of products and 620 of
+// other vector instructions; 560 workgroups make three wavefronts on some SIMDs, whose up to 3 x 18 such steps are the
+// call's 49 k cycles.
 // Slower: the wavefronts in two groups that take turns at products and softmax (288 to 309 us), 64 rows a wavefront with
 // one tile's softmax between another's products (322), wave priorities by phase and operands fetched 1 to 10 products ahead
 // (within 4 %).

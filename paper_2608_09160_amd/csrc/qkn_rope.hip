@@ -15,7 +15,8 @@
 //
 // Measured: 8192 tokens of 16 + 4 + 4 heads of 128 with the norm, bf16 cache, 105 MB: 24.6 us, 4.3 TB/s; 32768 tokens of
 // 16 + 2 + 2 heads into an FP8 cache, 337 MB: 71 us, 4.7 TB/s; a copy of as many bytes reaches 5 to 5.9. 64 tokens: 5.1 us, a
-// launch and one chain of latencies (position -> angles).
+// launch and one chain of latencies (position -> angles). Element by element (V = 1) 8192 tokens of 16 + 4 + 4 heads of 50, 41
+// MB, take 37.5 us; of 48, in vectors, 12.8.
 
 #include <string.h>
 
