@@ -233,7 +233,8 @@ class PreparedAttn:
     head_dim], the sequences in order) over the cache that holds their keys and values already.
 
     block_table int32 [batch, pages of a sequence], q_start int32 [batch + 1], kv_len int32 [batch] (new tokens
-    included) are read by the kernel on the device: a replayed graph sees what they hold then. max_q and max_kv: the
+    included) are read by the kernel on the device: a replayed graph sees what they hold then. Tokens before q_start's
+    first entry and behind its last are padding: out is 0 there, lse -infinity. max_q and max_kv: the
     largest numbers of new and cached tokens of a sequence (the default: T, and what block_table's rows can hold).
     lse: optional fp32 [T, heads], receives the log-sum-exp. window: keys that a token sees, its own the last (0:
     all)."""
