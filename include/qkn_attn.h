@@ -107,6 +107,17 @@ int64_t qkn_attn_workspace_bytes(const qkn_attn_args* args, const qkn_cache* cac
 int qkn_attn(const qkn_attn_args* args, const qkn_cache* cache, void* workspace, int64_t workspace_bytes,
              void* stream);
 
+/*
+ * Attention with the sequence's first `sinks` tokens visible whatever the
+ * window: token i sees, where window > 0, the keys j > m - n + i - window and
+ * the keys j < sinks, of those that it sees without a window. Anything else as
+ * for qkn_attn, which is the case sinks = 0; without a window sinks change
+ * nothing. The workspace is qkn_attn's for the same arguments. QKN_EINVAL also:
+ * sinks < 0.
+ */
+int qkn_attn_sinks(const qkn_attn_args* args, int32_t sinks, const qkn_cache* cache, void* workspace,
+                   int64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

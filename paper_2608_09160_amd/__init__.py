@@ -15,5 +15,6 @@ from ._lib import (QKN_EHIP, QKN_EINVAL, QKN_ENOTSUP, QKN_EOVERLAP, QKN_OK,  # n
                    Prepared, PreparedApply, PreparedPartial, QknError, Seg, load, qkn_apply, qkn_full, qkn_fused_shard,
                    qkn_fused_group_wait, qkn_fused_shard_wait, qkn_last_launch, qkn_partial_sumsq,
                    qkn_publish_partials, qkn_set_option, qkn_strerror)
-from ._serve import (AdapterSeg, KVCache, PreparedAdapters, PreparedAttn, PreparedRopeCache, RopeSeg,  # noqa: F401
-                     qkn_adapters_add, qkn_attn, qkn_rope_cache, qkn_rope_table)
+from ._serve import (AdapterSeg, KVCache, KVCache4, PreparedAdapters, PreparedAttn, PreparedCache4Load,  # noqa: F401
+                     PreparedRopeCache, RopeSeg, qkn_adapters_add, qkn_attn, qkn_cache4_load, qkn_rope_cache,
+                     qkn_rope_table)

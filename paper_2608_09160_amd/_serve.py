@@ -11,7 +11,7 @@ import contextlib
 import copy
 import ctypes
 from dataclasses import dataclass
-from typing import Optional
+from typing import Optional, Union
 
 import torch
 
@@ -25,6 +25,12 @@ class QknCache(ctypes.Structure):
                 ("page_size", ctypes.c_int32), ("n_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("fp8", ctypes.c_int32), ("k_page", _c_i64), ("k_head", _c_i64), ("k_token", _c_i64),
                 ("v_page", _c_i64), ("v_head", _c_i64), ("v_token", _c_i64)]
+
+
+class QknCache4(ctypes.Structure):
+    _fields_ = ([(n, _vp) for n in ("k", "v", "k_exp", "v_exp")] + [("num_pages", _c_i64)] +
+                [(n, ctypes.c_int32) for n in ("page_size", "n_kv", "head_dim")] +
+                [(f"{pool}_{n}", _c_i64) for pool in ("k", "v", "ke", "ve") for n in ("page", "head", "token")])
 
 
 class QknRopeScaling(ctypes.Structure):
@@ -58,6 +64,14 @@ def load() -> ctypes.CDLL:
         lib.qkn_rope_cache.argtypes = [ctypes.POINTER(QknRopeSeg), ctypes.POINTER(QknRopeSeg), _vp, _c_i64, _c_i64,
                                        _int, _int, _int, _vp, _c_i64, _vp, _vp, ctypes.POINTER(QknCache), _int,
                                        ctypes.c_float, _vp]
+        lib.qkn_rope_cache4.argtypes = [ctypes.POINTER(QknCache4) if a is ctypes.POINTER(QknCache) else a
+                                        for a in lib.qkn_rope_cache.argtypes]
+        lib.qkn_attn_sinks.argtypes = [ctypes.POINTER(QknAttnArgs), ctypes.c_int32, ctypes.POINTER(QknCache), _vp, _c_i64,
+                                       _vp]
+        lib.qkn_attn4_workspace_bytes.argtypes = [ctypes.POINTER(QknAttnArgs), ctypes.POINTER(QknCache4)]
+        lib.qkn_attn4_workspace_bytes.restype = _c_i64
+        lib.qkn_attn4.argtypes = [ctypes.POINTER(QknAttnArgs), ctypes.c_int32, ctypes.POINTER(QknCache4), _vp, _c_i64, _vp]
+        lib.qkn_cache4_load.argtypes = [ctypes.POINTER(QknCache4), _vp, _c_i64, _vp, _c_i64, _vp, _c_i64, _vp]
         lib.qkn_attn_workspace_bytes.argtypes = [ctypes.POINTER(QknAttnArgs), ctypes.POINTER(QknCache)]
         lib.qkn_attn_workspace_bytes.restype = _c_i64
         lib.qkn_attn.argtypes = [ctypes.POINTER(QknAttnArgs), ctypes.POINTER(QknCache), _vp, _c_i64, _vp]
@@ -88,6 +102,15 @@ def _index(t: torch.Tensor, what: str, dtype: torch.dtype, numel: int) -> int:
     return t.data_ptr()
 
 
+def _pool_strides(name: str, t: torch.Tensor) -> list:
+    """Strides of a page, a head and a token."""
+    D = t.shape[3]
+    if not t.is_cuda or (D > 1 and t.stride(3) != 1):
+        raise ValueError(f"cache.{name}: expected a GPU tensor with a contiguous last dimension")
+    # the stride of a dimension of one is never used
+    return [max(t.stride(i), D) if t.shape[i] == 1 else t.stride(i) for i in (0, 1, 2)]
+
+
 @dataclass
 class KVCache:
     """Pools of pages [pages, kv heads, page size, head dim], of any strides with a contiguous last dimension
@@ -104,14 +127,43 @@ class KVCache:
         if self.k.dim() != 4 or self.k.shape != self.v.shape:
             raise ValueError("cache: pools must be [pages, kv heads, page size, head dim], alike")
         pages, n_kv, page, D = self.k.shape
-        strides = []
-        for name, t in (("k", self.k), ("v", self.v)):
-            if not t.is_cuda or (D > 1 and t.stride(3) != 1):
-                raise ValueError(f"cache.{name}: expected a GPU tensor with a contiguous last dimension")
-            # the stride of a dimension of one is never used
-            strides += [max(t.stride(i), D) if t.shape[i] == 1 else t.stride(i) for i in (0, 1, 2)]
+        strides = _pool_strides("k", self.k) + _pool_strides("v", self.v)
         return QknCache(self.k.data_ptr(), self.v.data_ptr(), _f32(self.k_scale, "k_scale", n_kv),
                         _f32(self.v_scale, "v_scale", n_kv), pages, page, n_kv, D, _CACHE_DTYPES[self.k.dtype], *strides)
+
+
+@dataclass
+class KVCache4:
+    """Pools of a cache in 4 bits, uint8: codes [pages, kv heads, page size, head dim / 2], two to a byte, and exponents
+    [pages, kv heads, page size, head dim / 32] (include/qkn_cache4.h has the format); any strides with a contiguous last
+    dimension. Takes a KVCache's place in PreparedRopeCache and PreparedAttn; qkn_cache4_load reads rows back."""
+
+    k: torch.Tensor
+    v: torch.Tensor
+    k_exp: torch.Tensor
+    v_exp: torch.Tensor
+
+    @classmethod
+    def empty(cls, pages: int, kv_heads: int, page_size: int, head_dim: int, device="cuda") -> "KVCache4":
+        """Pools of that size, not cleared."""
+        return cls(*(torch.empty(pages, kv_heads, page_size, head_dim // n, dtype=torch.uint8, device=device)
+                     for n in (2, 2, 32, 32)))
+
+    @property
+    def head_dim(self) -> int:
+        return 2 * self.k.shape[3]
+
+    def struct(self) -> QknCache4:
+        pools = (self.k, self.v, self.k_exp, self.v_exp)
+        if any(t.dtype != torch.uint8 for t in pools):
+            raise TypeError(f"cache: expected four uint8 pools, got {[t.dtype for t in pools]}")
+        if self.k.dim() != 4 or self.k.shape[3] % 16:
+            raise ValueError("cache: codes must be [pages, kv heads, page size, head dim / 2], head dim a multiple of 32")
+        pages, n_kv, page, half = self.k.shape
+        if self.v.shape != self.k.shape or any(tuple(t.shape) != (pages, n_kv, page, half // 16) for t in pools[2:]):
+            raise ValueError("cache: pools must be of the same pages, heads and rows, exponents [.., head dim / 32]")
+        strides = [s for name, t in zip(("k", "v", "k_exp", "v_exp"), pools) for s in _pool_strides(name, t)]
+        return QknCache4(*(t.data_ptr() for t in pools), pages, page, n_kv, 2 * half, *strides)
 
 
 @dataclass
@@ -142,12 +194,13 @@ def qkn_rope_table(n_pos: int, rot_dim: int, base: float = 10000.0, factor: floa
 class PreparedRopeCache:
     """qkn_rope_cache with its arguments checked and marshalled once: Q and K rows (normalised first where a
     segment has w) rotated by pos (int32 [T]) with table, Q to q.y, K to k.y where given, K and V to rows `slots`
-    (int64 [T], page * page size + row; negative: not cached) of the cache. table None: no rotation."""
+    (int64 [T], page * page size + row; negative: not cached) of the cache (a KVCache4: quantised to 4 bits). table
+    None: no rotation."""
 
     def __init__(self, table: Optional[torch.Tensor], pos: Optional[torch.Tensor], head_dim: int,
                  q: Optional[RopeSeg] = None, k: Optional[RopeSeg] = None, v: Optional[torch.Tensor] = None,
-                 cache: Optional[KVCache] = None, slots: Optional[torch.Tensor] = None, interleaved: bool = False,
-                 eps: float = 1e-6):
+                 cache: Union[KVCache, KVCache4, None] = None, slots: Optional[torch.Tensor] = None,
+                 interleaved: bool = False, eps: float = 1e-6):
         if q is None and k is None:
             raise ValueError("q, k or both must be given")
         T, tp, segs = None, None, []
@@ -205,10 +258,11 @@ class PreparedRopeCache:
         ref = [ctypes.byref(s) if s is not None else None for s in segs]
         self._args = (ref[0], ref[1], pv, ldv, T, head_dim, rot, int(interleaved), pt, n_pos, pp, ps,
                       ctypes.byref(self._cache) if cache is not None else None, tp or 1, ctypes.c_float(eps))
-        self._fn = load().qkn_rope_cache
+        self._name = "qkn_rope_cache4" if isinstance(cache, KVCache4) else "qkn_rope_cache"
+        self._fn = getattr(load(), self._name)
 
     def __call__(self, stream=None):
-        _check(self._fn(*self._args, _stream(stream)), "qkn_rope_cache")
+        _check(self._fn(*self._args, _stream(stream)), self._name)
         return self.q.y if self.q is not None else None
 
 
@@ -228,7 +282,7 @@ def _workspace(workspace: Optional[torch.Tensor], need: int, device) -> torch.Te
 
 
 class PreparedAttn:
-    """qkn_attn with its arguments and workspace prepared once (calls share the workspace: on one stream at a time):
+    """qkn_attn (qkn_attn_sinks, qkn_attn4) with its arguments and workspace prepared once (calls share the workspace: on one stream at a time):
     attention of the new tokens q (bf16 [T, heads *
     head_dim], the sequences in order) over the cache that holds their keys and values already.
 
@@ -237,13 +291,13 @@ class PreparedAttn:
     first entry and behind its last are padding: out is 0 there, lse -infinity. max_q and max_kv: the
     largest numbers of new and cached tokens of a sequence (the default: T, and what block_table's rows can hold).
     lse: optional fp32 [T, heads], receives the log-sum-exp. window: keys that a token sees, its own the last (0:
-    all)."""
+    all); sinks: the sequence's first tokens, which it sees as well. cache may be a KVCache4."""
 
-    def __init__(self, q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, q_start: torch.Tensor,
+    def __init__(self, q: torch.Tensor, cache: Union[KVCache, KVCache4], block_table: torch.Tensor, q_start: torch.Tensor,
                  kv_len: torch.Tensor, max_q: Optional[int] = None, max_kv: Optional[int] = None,
                  scale: Optional[float] = None, causal: bool = True, window: int = 0,
                  out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
-                 workspace: Optional[torch.Tensor] = None):
+                 workspace: Optional[torch.Tensor] = None, sinks: int = 0):
         c = cache.struct()
         pq, ldq, T, width = _rows(q, "q")
         if width % c.head_dim or (width // c.head_dim) % c.n_kv:
@@ -269,26 +323,63 @@ class PreparedAttn:
                         _index(block_table, "block_table", torch.int32, batch * pages), pages, T, batch, heads, max_q,
                         max_kv, int(causal), window, c.head_dim ** -0.5 if scale is None else scale)
         lib = load()
-        need = lib.qkn_attn_workspace_bytes(ctypes.byref(a), ctypes.byref(c))
+        name = "qkn_attn4" if isinstance(cache, KVCache4) else "qkn_attn"
+        need = getattr(lib, name + "_workspace_bytes")(ctypes.byref(a), ctypes.byref(c))
         if need < 0:
-            _check(int(need), "qkn_attn_workspace_bytes")
+            _check(int(need), name + "_workspace_bytes")
+        self._name = name if name == "qkn_attn4" else "qkn_attn_sinks"
         self.workspace = _workspace(workspace, need, q.device)
         self.q, self.out, self.lse, self.cache = q, out, lse, copy.copy(cache)
         self._keep = (block_table, q_start, kv_len, a, c)
-        self._args = (ctypes.byref(a), ctypes.byref(c), self.workspace.data_ptr(), self.workspace.numel())
-        self._fn = lib.qkn_attn
+        self._args = (ctypes.byref(a), sinks, ctypes.byref(c), self.workspace.data_ptr(), self.workspace.numel())
+        self._fn = getattr(lib, self._name)
 
     def __call__(self, stream=None) -> torch.Tensor:
-        _check(self._fn(*self._args, _stream(stream)), "qkn_attn")
+        _check(self._fn(*self._args, _stream(stream)), self._name)
         return self.out
 
 
 def qkn_attn(q, cache, block_table, q_start, kv_len, max_q=None, max_kv=None, scale=None, causal=True, window=0,
-             out=None, lse=None, workspace=None, stream=None) -> torch.Tensor:
+             out=None, lse=None, workspace=None, stream=None, sinks=0) -> torch.Tensor:
     """PreparedAttn made and called once."""
     with _on(stream):
         return PreparedAttn(q, cache, block_table, q_start, kv_len, max_q, max_kv, scale, causal, window, out, lse,
-                            workspace)()
+                            workspace, sinks)()
+
+
+class PreparedCache4Load:
+    """qkn_cache4_load with its arguments prepared once: the rows `slots` (int64 [T], page * page size + row; outside the
+    cache: zeros) of a 4-bit cache as bf16 [T, kv heads * head_dim], to k and v (allocated if both are None)."""
+
+    def __init__(self, cache: KVCache4, slots: torch.Tensor, k: Optional[torch.Tensor] = None,
+                 v: Optional[torch.Tensor] = None):
+        c, T = cache.struct(), slots.numel()
+        width = c.n_kv * c.head_dim
+        if k is None and v is None:
+            k, v = (torch.empty(T, width, dtype=torch.bfloat16, device=slots.device) for _ in range(2))
+        rows = []
+        for name, t in (("k", k), ("v", v)):
+            if t is None:
+                rows += [None, 0]
+                continue
+            p, ld, Tt, w = _rows(t, name)
+            if (Tt, w) != (T, width):
+                raise ValueError(f"{name}: expected [{T}, {width}]")
+            rows += [p, ld]
+        self.k, self.v, self.cache = k, v, copy.copy(cache)
+        self._keep = (slots, c)
+        self._args = (ctypes.byref(c), _index(slots, "slots", torch.int64, T), T, *rows)
+        self._fn = load().qkn_cache4_load
+
+    def __call__(self, stream=None):
+        _check(self._fn(*self._args, _stream(stream)), "qkn_cache4_load")
+        return self.k, self.v
+
+
+def qkn_cache4_load(cache, slots, k=None, v=None, stream=None):
+    """PreparedCache4Load made and called once; returns (k, v)."""
+    with _on(stream):
+        return PreparedCache4Load(cache, slots, k, v)()
 
 
 @dataclass

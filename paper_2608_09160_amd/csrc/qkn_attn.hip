@@ -5,6 +5,7 @@
 
 #include "qkn_attn.h"
 #include "qkn_attn_kernels.h"
+#include "qkn_cache4.h"
 
 namespace attn {
 
@@ -104,25 +105,68 @@ struct Plan {
   bool split;
 };
 
+// A cache of any format.
+struct Source {
+  Format format;
+  bool ok;                                      // its sizes and strides
+  int64_t num_pages;
+  int32_t page_size, n_kv, head_dim, multiple;  // of head_dim
+  Pool k, v;                                    // strides in bytes
+  Exponents ke, ve;
+  Span spans[4];                                // the pools; scales or exponents
+
+  explicit Source(const qkn_cache& c)
+      : format(c.fp8 ? kFp8 : kBf16), ok(cache_ok(c)), num_pages(c.num_pages), page_size(c.page_size), n_kv(c.n_kv),
+        head_dim(c.head_dim), multiple(c.fp8 ? 16 : 8), ke{}, ve{}, spans{} {
+    if (!ok) return;
+    const int64_t esz = c.fp8 ? 1 : 2;
+    k = Pool{static_cast<const unsigned char*>(c.k), c.k_scale, c.k_page * esz, c.k_head * esz, static_cast<uint32_t>(c.k_token * esz)};
+    v = Pool{static_cast<const unsigned char*>(c.v), c.v_scale, c.v_page * esz, c.v_head * esz, static_cast<uint32_t>(c.v_token * esz)};
+    spans[0] = pool_span(c, c.k, c.k_page, c.k_head, c.k_token);
+    spans[1] = pool_span(c, c.v, c.v_page, c.v_head, c.v_token);
+    spans[2] = array_span(c.k_scale, c.n_kv, 4);
+    spans[3] = array_span(c.v_scale, c.n_kv, 4);
+    widest = (c.k_token > c.v_token ? c.k_token : c.v_token) * esz;
+  }
+  explicit Source(const qkn_cache4& c)
+      : format(kFp4), ok(cache4_ok(c)), num_pages(c.num_pages), page_size(c.page_size), n_kv(c.n_kv), head_dim(c.head_dim),
+        multiple(32), ke{}, ve{}, spans{} {
+    if (!ok) return;
+    k = Pool{c.k, nullptr, c.k_page, c.k_head, static_cast<uint32_t>(c.k_token)};
+    v = Pool{c.v, nullptr, c.v_page, c.v_head, static_cast<uint32_t>(c.v_token)};
+    ke = Exponents{c.k_exp, c.ke_page, c.ke_head, static_cast<uint32_t>(c.ke_token)};
+    ve = Exponents{c.v_exp, c.ve_page, c.ve_head, static_cast<uint32_t>(c.ve_token)};
+    for (int i = 0; i < 4; ++i) spans[i] = pool4_span(c, i);
+    widest = 0;
+    for (int64_t t : {c.k_token, c.v_token, c.ke_token, c.ve_token}) widest = t > widest ? t : widest;
+  }
+  int64_t widest;  // stride of a token, bytes
+  bool pools_given() const { return k.base && v.base && (format != kFp4 || (ke.base && ve.base)); }
+  bool vectors() const {  // exponents are read byte by byte
+    for (const Pool* x : {&k, &v})
+      if (!aligned(x->base, 16) || x->page % 16 || x->head % 16 || x->token % 16) return false;
+    return true;
+  }
+};
+
 // Sizes alone: QKN_OK, QKN_EINVAL or QKN_ENOTSUP.
-int check_sizes(const qkn_attn_args* a, const qkn_cache* c) {
-  if (!a || !c || !cache_ok(*c) || a->T < 0 || a->batch < 0 || a->max_q < 0 || a->max_kv < 0 || a->n_q < 1 ||
+int check_sizes(const qkn_attn_args* a, int32_t sinks, const Source* c) {
+  if (!a || !c || !c->ok || sinks < 0 || a->T < 0 || a->batch < 0 || a->max_q < 0 || a->max_kv < 0 || a->n_q < 1 ||
       a->n_q % c->n_kv || a->ld_table < 0 || a->window < 0 || (a->window && !a->causal) || !(a->scale > 0.0f) ||
       isinf(a->scale))
     return QKN_EINVAL;
   const int64_t width = static_cast<int64_t>(a->n_q) * c->head_dim;
   if (a->ldq < width || a->ldo < width) return QKN_EINVAL;
-  const int64_t lim = int64_t{1} << 31, esz = c->fp8 ? 1 : 2, group = a->n_q / c->n_kv;
-  if (c->head_dim > 256 || c->head_dim % (c->fp8 ? 16 : 8) || c->page_size < 16 || a->T >= lim || a->n_q >= lim / 8 ||
+  const int64_t lim = int64_t{1} << 31, group = a->n_q / c->n_kv;
+  if (c->head_dim > 256 || c->head_dim % c->multiple || c->page_size < 16 || a->T >= lim || a->n_q >= lim / 8 ||
       a->T * a->n_q >= lim || a->T * group + int64_t{a->batch} * 512 >= lim || a->ld_table > lim ||
-      a->ld_table * c->page_size > lim - (1 << 17) || c->k_token * esz * c->page_size >= lim ||
-      c->v_token * esz * c->page_size >= lim)
+      a->ld_table * c->page_size > lim - (1 << 17) || c->widest * c->page_size >= lim)
     return QKN_ENOTSUP;
   return QKN_OK;
 }
 
 // The workgroups of kernel v, and their workspace.
-Plan plan_with(const qkn_attn_args& a, const qkn_cache& c, const Variant& v) {
+Plan plan_with(const qkn_attn_args& a, const Source& c, const Variant& v) {
   Plan pl{};
   pl.v = v;
   const int64_t group = a.n_q / c.n_kv;
@@ -146,44 +190,51 @@ Plan plan_with(const qkn_attn_args& a, const qkn_cache& c, const Variant& v) {
   return pl;
 }
 
+Variant few_rows_of(const Source& c, bool sinks, int dt, int rows) {
+  if (c.format == kFp4) return few_rows4(dt, rows);
+  return (sinks ? few_rows_sinks : few_rows)(dt, c.format == kFp8, rows);
+}
+Variant many_rows_of(const Source& c, bool sinks, int dt, bool small) {
+  if (c.format == kFp4) return many_rows4(dt, small);
+  return (sinks ? many_rows_sinks : many_rows)(dt, c.format == kFp8, small);
+}
+
 // The kernel, of two that may serve where rows are many: little work, or much.
-Plan plan_of(const qkn_attn_args& a, const qkn_cache& c, int64_t* workspace_bytes = nullptr) {
+Plan plan_of(const qkn_attn_args& a, int32_t sinks, const Source& c, int64_t* workspace_bytes = nullptr) {
   const int dt = c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256;
   const int64_t group = a.n_q / c.n_kv, rows = (a.max_q < 1 ? 1 : a.max_q) * group;
   const bool few = rows <= (dt == 256 ? 32 : 64);
   if (few) {
-    const Plan pl = plan_with(a, c, few_rows(dt, c.fp8 != 0, static_cast<int>(rows)));
+    const Plan pl = plan_with(a, c, few_rows_of(c, sinks, dt, static_cast<int>(rows)));
     if (workspace_bytes) *workspace_bytes = pl.ws_bytes;
     return pl;
   }
   // keys that a row sees, about, and pairs of 64 rows and 64 keys in all
   int64_t keys = a.max_kv - (a.causal ? (a.max_q < a.max_kv ? a.max_q : a.max_kv) / 2 : 0);
-  if (a.window && a.window < keys) keys = a.window;
+  if (a.window && int64_t{a.window} + sinks < keys) keys = int64_t{a.window} + sinks;
   const int64_t pairs = (a.T * group + 63) / 64 * c.n_kv * ((keys + 63) / 64);
-  const Plan small = plan_with(a, c, many_rows(dt, c.fp8 != 0, true)), large = plan_with(a, c, many_rows(dt, c.fp8 != 0, false));
+  const Plan small = plan_with(a, c, many_rows_of(c, sinks, dt, true)), large = plan_with(a, c, many_rows_of(c, sinks, dt, false));
   // the mask chooses between them, not the workspace: one serves a model's layers with and without a window
   if (workspace_bytes) *workspace_bytes = small.ws_bytes > large.ws_bytes ? small.ws_bytes : large.ws_bytes;
   return pairs <= kSmallPairs ? small : large;
 }
 
-int attn_impl(const qkn_attn_args* args, const qkn_cache* cache, void* workspace, int64_t workspace_bytes,
+int attn_impl(const qkn_attn_args* args, int32_t sinks, const Source* cache, void* workspace, int64_t workspace_bytes,
               void* stream) {
-  int rc = check_sizes(args, cache);
+  int rc = check_sizes(args, sinks, cache);
   if (rc != QKN_OK) return rc;
   const qkn_attn_args& a = *args;
-  const qkn_cache& c = *cache;
+  const Source& c = *cache;
+  if (!a.window) sinks = 0;  // every token sees them
   if (a.T == 0) return QKN_OK;
   if (!a.q || !a.out || !a.q_start || (a.batch && (!a.kv_len || (a.ld_table && !a.block_table))) ||
-      (c.num_pages && (!c.k || !c.v)))
+      (c.num_pages && !c.pools_given()))
     return QKN_EINVAL;
-  const Plan pl = plan_of(a, c);
+  const Plan pl = plan_of(a, sinks, c);
   if (pl.ws_bytes && (!workspace || workspace_bytes < pl.ws_bytes)) return QKN_EINVAL;
-  const int64_t esz = c.fp8 ? 1 : 2, per = 16 / esz;
-  if (!aligned(a.q, 16) || !aligned(a.out, 16) || a.ldq % 8 || a.ldo % 8 || !aligned(c.k, 16) || !aligned(c.v, 16) ||
+  if (!aligned(a.q, 16) || !aligned(a.out, 16) || a.ldq % 8 || a.ldo % 8 || !c.vectors() ||
       (pl.ws_bytes && !aligned(workspace, 16)))
     return QKN_ENOTSUP;
-  for (int64_t s : {c.k_page, c.k_head, c.k_token, c.v_page, c.v_head, c.v_token})
-    if (s % per) return QKN_ENOTSUP;
   const int64_t rows = a.T * a.n_q;
   if (pl.grid >= int64_t{1} << 31) return QKN_ENOTSUP;
 
@@ -192,10 +243,7 @@ int attn_impl(const qkn_attn_args* args, const qkn_cache* cache, void* workspace
                      array_span(a.q_start, int64_t{a.batch} + 1, 4),
                      array_span(a.kv_len, a.batch, 4),
                      array_span(a.block_table, a.batch * a.ld_table, 4),
-                     pool_span(c, c.k, c.k_page, c.k_head, c.k_token),
-                     pool_span(c, c.v, c.v_page, c.v_head, c.v_token),
-                     array_span(c.k_scale, c.n_kv, 4),
-                     array_span(c.v_scale, c.n_kv, 4)};
+                     c.spans[0], c.spans[1], c.spans[2], c.spans[3]};
   const Span out[] = {Span{reinterpret_cast<uintptr_t>(a.out), a.T, a.ldo, width, 2}, array_span(a.lse, rows, 4),
                       array_span(pl.ws_bytes ? workspace : nullptr, pl.ws_bytes, 1)};
   for (int i = 0; i < 3; ++i) {
@@ -217,10 +265,10 @@ int attn_impl(const qkn_attn_args* args, const qkn_cache* cache, void* workspace
   p.ldo = a.ldo;
   p.ld_table = a.ld_table;
   p.T = a.T;
-  p.k = Pool{static_cast<const unsigned char*>(c.k), c.k_scale, c.k_page * esz, c.k_head * esz,
-             static_cast<uint32_t>(c.k_token * esz)};
-  p.v = Pool{static_cast<const unsigned char*>(c.v), c.v_scale, c.v_page * esz, c.v_head * esz,
-             static_cast<uint32_t>(c.v_token * esz)};
+  p.k = c.k;
+  p.v = c.v;
+  p.ke = c.ke;
+  p.ve = c.ve;
   p.num_pages = static_cast<uint32_t>(c.num_pages);
   p.page_shift = log2_of(c.page_size);
   p.batch = a.batch;
@@ -230,6 +278,7 @@ int attn_impl(const qkn_attn_args* args, const qkn_cache* cache, void* workspace
   p.items = static_cast<int32_t>(pl.items);
   p.causal = a.causal != 0;
   p.window = a.window;
+  p.sinks = sinks;
   p.c = a.scale * 1.44269504088896340736f;
   p.group = fast_div(static_cast<uint32_t>(a.n_q / c.n_kv));
   p.kv_heads = fast_div(static_cast<uint32_t>(c.n_kv));
@@ -264,22 +313,48 @@ int attn_impl(const qkn_attn_args* args, const qkn_cache* cache, void* workspace
   return QKN_OK;
 }
 
+int64_t workspace_bytes_of(const qkn_attn_args* args, const Source* cache) {
+  const int rc = check_sizes(args, 0, cache);
+  if (rc != QKN_OK) return rc;
+  if (args->T == 0) return 0;
+  int64_t bytes = 0;
+  plan_of(*args, 0, *cache, &bytes);
+  return bytes;
+}
+
 }  // namespace attn
 
 extern "C" {
 
 int64_t qkn_attn_workspace_bytes(const qkn_attn_args* args, const qkn_cache* cache) {
-  const int rc = attn::check_sizes(args, cache);
-  if (rc != QKN_OK) return rc;
-  if (args->T == 0) return 0;
-  int64_t bytes = 0;
-  attn::plan_of(*args, *cache, &bytes);
-  return bytes;
+  if (!cache) return QKN_EINVAL;
+  const attn::Source c(*cache);
+  return attn::workspace_bytes_of(args, &c);
 }
 
 int qkn_attn(const qkn_attn_args* args, const qkn_cache* cache, void* workspace, int64_t workspace_bytes,
              void* stream) {
-  return attn::attn_impl(args, cache, workspace, workspace_bytes, stream);
+  return qkn_attn_sinks(args, 0, cache, workspace, workspace_bytes, stream);
+}
+
+int qkn_attn_sinks(const qkn_attn_args* args, int32_t sinks, const qkn_cache* cache, void* workspace,
+                   int64_t workspace_bytes, void* stream) {
+  if (!cache) return QKN_EINVAL;
+  const attn::Source c(*cache);
+  return attn::attn_impl(args, sinks, &c, workspace, workspace_bytes, stream);
+}
+
+int64_t qkn_attn4_workspace_bytes(const qkn_attn_args* args, const qkn_cache4* cache) {
+  if (!cache) return QKN_EINVAL;
+  const attn::Source c(*cache);
+  return attn::workspace_bytes_of(args, &c);
+}
+
+int qkn_attn4(const qkn_attn_args* args, int32_t sinks, const qkn_cache4* cache, void* workspace,
+              int64_t workspace_bytes, void* stream) {
+  if (!cache) return QKN_EINVAL;
+  const attn::Source c(*cache);
+  return attn::attn_impl(args, sinks, &c, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

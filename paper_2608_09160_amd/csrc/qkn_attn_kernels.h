@@ -48,6 +48,7 @@
 #define QKN_ATTN_KERNELS_H
 
 #include "qkn_block.h"
+#include "qkn_quant4.h"
 
 namespace attn {
 
@@ -66,6 +67,12 @@ struct Pool {
   uint32_t token;
 };
 
+struct Exponents {  // of a 4-bit pool
+  const unsigned char* base;
+  int64_t page, head;
+  uint32_t token;
+};
+
 struct Params {
   const uint16_t* q;
   uint16_t* out;
@@ -75,11 +82,12 @@ struct Params {
   const int32_t* table;
   int64_t ldq, ldo, ld_table, T;
   Pool k, v;
+  Exponents ke, ve;
   uint32_t num_pages;
   int32_t page_shift;
   int32_t batch, n_q, n_kv, D;
   int32_t items;                       // workgroups of a KV head
-  int32_t causal, window;
+  int32_t causal, window, sinks;
   float c;                             // scale * log2(e)
   FastDiv group, kv_heads;
   // split keys (NULL: not split): what each workgroup has of its row tile, and which workgroups have a row's parts
@@ -122,11 +130,15 @@ __device__ __forceinline__ void group_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// DT: head size, rounded up (the rest reads as zeros); OCC: wavefronts per SIMD that the registers must allow.
-template <int DT_, bool FP8_, int CB_, int WAVES_, bool SHARED_, int KT_, int OCC_>
+// What the cache holds.
+enum Format { kBf16, kFp8, kFp4 };
+
+// DT: head size, rounded up (the rest reads as zeros); OCC: wavefronts per SIMD that the registers must allow. SINKS: rows
+// may see the sequence's first keys besides their window.
+template <int DT_, int FMT, int CB_, int WAVES_, bool SHARED_, int KT_, int OCC_, bool SINKS_>
 struct Cfg {
   static constexpr int DT = DT_, CB = CB_, WAVES = WAVES_, KT = KT_, OCC = OCC_;
-  static constexpr bool FP8 = FP8_, SHARED = SHARED_;
+  static constexpr bool FP8 = FMT == kFp8, FP4 = FMT == kFp4, SHARED = SHARED_, SINKS = SINKS_;
   static constexpr int AHEAD = 4;                 // LDS reads ahead of their products
   static constexpr int ES = FP8 ? 1 : 2;
   static constexpr int RB = DT * ES;              // bytes of an LDS row
@@ -138,14 +150,19 @@ struct Cfg {
   static constexpr int BUF = (SHARED ? 2 : 1) * TILE;  // a buffer: K and V, or V
   static constexpr int V_AT = SHARED ? TILE : 0;  // V in it
   static constexpr int STEP = KT * (SHARED ? 1 : WAVES);  // keys that a workgroup takes at a time
-  static constexpr int KL = DT * ES / 64;         // 16-byte loads of 16 K rows into registers (!SHARED)
+  static constexpr int KL = FP4 ? (DT == 256 ? 2 : 1) : DT * ES / 64;  // loads of 16 K rows into registers (!SHARED)
   static constexpr int BR = SHARED ? KT / WAVES : 16;  // rows that a wavefront loads together, of one page
   static constexpr int BLOCKS = SHARED ? 1 : KT / 16;  // how often for a tile
   static constexpr int V_LOADS = BLOCKS * BR / RPL;    // load instructions of a wavefront for a V tile
   static constexpr int STAGES = SHARED ? 1 : WAVES;    // key streams of a workgroup
+  static constexpr int BUFFERS = FP4 && !SHARED ? 1 : 2;
+  // FP4: a lane takes 16 bytes of codes (heads of 64: 8) and the exponent of their 32 (16) elements
+  static constexpr int LANE_CODES = DT == 64 ? 8 : 16, ROW_LANES = DT / 2 / LANE_CODES;
+  static constexpr int CODE_LOADS = ROW_LANES / 4;     // load instructions for 16 rows
+  static constexpr int CODE_WORDS = LANE_CODES / 4;    // a lane's words of a load: 8 elements each
   static constexpr int JOIN_ROW = DT + 4;         // floats of a row while wavefronts are joined
   static constexpr int JOIN = SHARED ? 0 : WAVES * 16 * CB * (JOIN_ROW + 2) * 4;
-  static constexpr int LDS = 2 * BUF * STAGES > JOIN ? 2 * BUF * STAGES : JOIN;
+  static constexpr int LDS = BUFFERS * BUF * STAGES > JOIN ? BUFFERS * BUF * STAGES : JOIN;
   static_assert(BR % RPL == 0, "whole load instructions");
   static_assert(WAVES == 4, "a wavefront of a workgroup on each SIMD");
   static constexpr int SLOTS = OCC < 160 * 1024 / LDS ? OCC : 160 * 1024 / LDS;  // workgroups that a CU holds
@@ -197,8 +214,12 @@ struct Tiles {
   const int32_t* table;     // the sequence's pages
   int32_t last_page;        // last entry in use
   int32_t page0;            // pages held: lane i has the bytes to page entry page0 + i (lower, upper half; < 0: none)
-  int32_t k_lo, k_hi, v_lo, v_hi;
+  int32_t k_lo, k_hi, v_lo, v_hi;  // FP4: k_lo the page's number
   int32_t next;             // and entry page0 + 64 + i
+  // SINKS: the rows' first keys end in page `sink_page`, their windows begin in page `near_page`; `next` is of next0
+  int32_t sink_page, near_page, next0;
+  const unsigned char* base_ke;  // FP4: the head's exponents of page 0
+  const unsigned char* base_ve;
 
   __device__ __forceinline__ Tiles(const Params& pp, unsigned char* b, int l, int w) : buf(b), lane(l), wave(w), p(pp) {}
 
@@ -208,6 +229,10 @@ struct Tiles {
   }
   // Takes 64 pages' places at once, a lane each: the address of a tile is then a few scalar instructions.
   __device__ __forceinline__ void hold(int32_t page) {
+    if constexpr (C::FP4) {
+      k_lo = page;
+      return;
+    }
     const bool none = static_cast<uint32_t>(page) >= p.num_pages;
     const int64_t k = none ? -1 : page * p.k.page, v = none ? -1 : page * p.v.page;
     k_lo = static_cast<int32_t>(k);
@@ -215,26 +240,45 @@ struct Tiles {
     v_lo = static_cast<int32_t>(v);
     v_hi = static_cast<int32_t>(v >> 32);
   }
-  __device__ __forceinline__ void open(int b, int head, int32_t m, int32_t first_key) {
+  // The 64 pages behind those from page `p0` on that the rows need.
+  __device__ __forceinline__ int32_t after(int32_t p0) const {
+    if constexpr (C::SINKS) return p0 + 64 > sink_page && p0 + 64 < near_page ? near_page : p0 + 64;
+    else return p0 + 64;
+  }
+  // sink_keys: the tiles of the first keys end there (0: none); near_key: the windows' begin there.
+  __device__ __forceinline__ void open(int b, int head, int32_t m, int32_t first_key, int32_t sink_keys, int32_t near_key) {
     base_k = p.k.base + head * p.k.head;
     base_v = p.v.base + head * p.v.head;
+    if constexpr (C::FP4) {
+      base_ke = p.ke.base + head * p.ke.head;
+      base_ve = p.ve.base + head * p.ve.head;
+    }
+    if constexpr (C::SINKS) {
+      sink_page = (sink_keys - 1) >> p.page_shift;
+      near_page = near_key >> p.page_shift;
+    }
     kv_len = m;
     table = p.table + b * p.ld_table;
     last_page = (m - 1) >> p.page_shift;
     page0 = first_key >> p.page_shift;
     const int32_t first = entry(page0 + lane);
-    next = entry(page0 + 64 + lane);
+    next0 = after(page0);
+    next = entry(next0 + lane);
     hold(first);
+  }
+  __device__ __forceinline__ void hold_for(int32_t page) {
+    while (page - page0 >= 64) {  // pages are taken in ascending order
+      hold(next);
+      page0 = next0;
+      next0 = after(page0);
+      next = entry(next0 + lane);
+    }
   }
   // The BR rows of K (V) from key j on, which are in one page: a descriptor of those that the sequence has.
   template <bool V>
   __device__ __forceinline__ Rsrc rows_of(int32_t j) {
     const int32_t pi = j >> p.page_shift;
-    while (pi - page0 >= 64) {  // pages are taken in ascending order
-      hold(next);
-      page0 += 64;
-      next = entry(page0 + 64 + lane);
-    }
+    hold_for(pi);
     const int32_t lo = __builtin_amdgcn_readlane(V ? v_lo : k_lo, pi - page0);
     const int32_t hi = __builtin_amdgcn_readlane(V ? v_hi : k_hi, pi - page0);
     const uint32_t token = V ? p.v.token : p.k.token, row0 = j & ((1 << p.page_shift) - 1);
@@ -245,6 +289,74 @@ struct Tiles {
     // a scalar, as it is the same on all lanes: a descriptor in vector registers costs a loop around every load
     const uint32_t bytes = __builtin_amdgcn_readfirstlane(none ? 0 : rows * token - (token - p.D * C::ES));
     return rsrc((V ? base_v : base_k) + (none ? 0 : off), bytes);
+  }
+  // FP4: 16 rows' codes and exponents, as one lane's part of a load.
+  struct Codes {
+    u32x4 w[C::CODE_LOADS];
+    uint32_t e[C::CODE_LOADS];
+  };
+  // FP4: descriptors of the 16 rows' codes and exponents from key j on.
+  template <bool V>
+  __device__ __forceinline__ void rows4_of(int32_t j, Rsrc& codes, Rsrc& exps) {
+    const int32_t pi = j >> p.page_shift;
+    hold_for(pi);
+    const uint32_t page = static_cast<uint32_t>(__builtin_amdgcn_readlane(k_lo, pi - page0));
+    const int64_t row0 = j & ((1 << p.page_shift) - 1);
+    const int32_t left = kv_len - j, rows = left < 16 ? left : 16;
+    const bool none = left <= 0 || page >= p.num_pages;
+    const Pool& c = V ? p.v : p.k;
+    const Exponents& e = V ? p.ve : p.ke;
+    const uint32_t c_bytes = __builtin_amdgcn_readfirstlane(none ? 0 : rows * c.token - (c.token - p.D / 2));
+    const uint32_t e_bytes = __builtin_amdgcn_readfirstlane(none ? 0 : rows * e.token - (e.token - p.D / 32));
+    codes = rsrc((V ? base_v : base_k) + (none ? 0 : page * c.page + row0 * c.token), c_bytes);
+    exps = rsrc((V ? base_ve : base_ke) + (none ? 0 : page * e.page + row0 * e.token), e_bytes);
+  }
+  // Byte `at` of row r's codes, the exponent with it; past the head's end zeros.
+  template <bool V>
+  __device__ __forceinline__ void load4(Rsrc codes, Rsrc exps, int r, uint32_t at, u32x4& w, uint32_t& e) const {
+    const bool in = at < static_cast<uint32_t>(p.D / 2);
+    const uint32_t from = in ? r * (V ? p.v.token : p.k.token) + at : 0x7fffffffu;
+    if constexpr (C::LANE_CODES == 16) {
+      w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, from, 0, 0));
+    } else {
+      const u32x2 u = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, from, 0, 0));
+      w = u32x4{u[0], u[1], 0u, 0u};
+    }
+    e = __builtin_amdgcn_raw_buffer_load_b8(exps, in ? r * (V ? p.ve.token : p.ke.token) + at / 16 : 0x7fffffffu, 0, 0);
+  }
+  // Requests the 16 rows from key j on; lane l has part l % ROW_LANES of row l / ROW_LANES (+ 64 / ROW_LANES a load).
+  template <bool V>
+  __device__ __forceinline__ void fetch(int32_t j, Codes& x) {
+    Rsrc codes, exps;
+    rows4_of<V>(j, codes, exps);
+#pragma unroll
+    for (int i = 0; i < C::CODE_LOADS; ++i)
+      load4<V>(codes, exps, i * (64 / C::ROW_LANES) + lane / C::ROW_LANES, lane % C::ROW_LANES * C::LANE_CODES, x.w[i], x.e[i]);
+  }
+  // Writes such rows as bf16, row row0 of the K (V) tile in buffer `at` on. `finite`: 0 in the place of NaN; true if
+  // there was any.
+  template <bool V>
+  __device__ __forceinline__ bool put(const Codes& x, int row0, int at, bool finite) {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < C::CODE_LOADS; ++i) {
+      const int r = row0 + i * (64 / C::ROW_LANES) + lane / C::ROW_LANES;
+      unsigned char* row = buf + at * C::BUF + (V ? C::V_AT : 0) + r * C::RB;
+      const int chunk0 = lane % C::ROW_LANES * C::CODE_WORDS, swizzle = V ? C::swizzle_v(r) : C::swizzle_k(r);
+      const bool nan = x.e[i] == 255;
+      const bool some = __builtin_amdgcn_ballot_w64(nan);
+      any |= some;
+#pragma unroll
+      for (int e = 0; e < C::CODE_WORDS; ++e) {
+        u32x4 u = __builtin_bit_cast(u32x4, quant4::decode(x.w[i][e], x.e[i]));
+        if (some && nan) {
+          const uint32_t two = finite ? 0u : 0x7fc07fc0u;
+          u = u32x4{two, two, two, two};
+        }
+        *reinterpret_cast<u32x4*>(row + ((chunk0 + e) ^ swizzle) * 16) = u;
+      }
+    }
+    return any;
   }
   __device__ __forceinline__ int first_row(int bl) const { return C::BR * (C::SHARED ? wave : bl); }
   // Requests this wavefront's rows of the K (V) tile at key j0 into buffer `at`.
@@ -278,10 +390,22 @@ struct Tiles {
       }
     }
   }
+  // FP4: the same; lane l has its codes of row l mod 16, bytes LANE_CODES (l / 16) .. of each 64 (heads of 64: 32).
+  __device__ __forceinline__ void request_k4(int32_t j0, u32x4 (&k)[C::KT / 16][C::KL], uint32_t (&e)[C::KT / 16][C::KL]) {
+#pragma unroll
+    for (int bl = 0; bl < C::KT / 16; ++bl) {
+      Rsrc codes, exps;
+      rows4_of<false>(j0 + 16 * bl, codes, exps);
+#pragma unroll
+      for (int x = 0; x < C::KL; ++x)
+        load4<false>(codes, exps, lane & 15, C::LANE_CODES * (4 * x + (lane >> 4)), k[bl][x], e[bl][x]);
+    }
+  }
   // A weight of 0 times an infinite or NaN value is NaN, which a row that does not see the key must not get. In a
   // tile that some rows see in part the product takes 0 in the place of such values (add_infinities gives them to the
   // rows that see them): puts it there in the V rows that this wavefront fetched; true if it found any.
   __device__ __forceinline__ bool make_finite(int at) {
+
     bool any = false;
 #pragma unroll
     for (int bl = 0; bl < C::BLOCKS; ++bl)
@@ -366,7 +490,8 @@ struct Rows {
   bf16x8 q[C::DT / 32][C::CB];
   f32x4 o[C::DT / 16][C::CB];   // O^T, this lane's elements 16 db + 4 (lane / 16) .. + 3
   float m[C::CB], l[C::CB];     // bound (of raw scores); sum over this lane's keys
-  int32_t lo[C::CB], hi[C::CB]; // the keys that the row sees
+  int32_t lo[C::CB], hi[C::CB]; // the keys that the row sees,
+  int32_t first[C::CB];         // and (SINKS) those before this one
 };
 
 template <class C>
@@ -376,8 +501,8 @@ using Weights = bf16x8[C::KT / 32][C::CB];
 
 // S^T = K Q^T of the tile in buffer `at` (!SHARED: of the K rows in kr).
 template <class C>
-__device__ __forceinline__ void scores(const Tiles<C>& t, const Rows<C>& w, const u32x4 (&kr)[C::KT / 16][C::KL], int at,
-                                       Scores<C>& s) {
+__device__ __forceinline__ void scores(const Tiles<C>& t, const Rows<C>& w, const u32x4 (&kr)[C::KT / 16][C::KL],
+                                       const uint32_t (&ke)[C::KT / 16][C::KL], int at, Scores<C>& s) {
   constexpr int KB = C::KT / 16, NS = C::DT / 32;
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb)
@@ -398,6 +523,8 @@ __device__ __forceinline__ void scores(const Tiles<C>& t, const Rows<C>& w, cons
     if constexpr (C::SHARED) {
       if (n < NS * KB) a[n % RING] = t.k_frag(at, n % KB, n / KB);
       f = Tiles<C>::operand(a[i % RING]);
+    } else if constexpr (C::FP4) {
+      f = quant4::decode(kr[kb][step / C::CODE_WORDS][step % C::CODE_WORDS], ke[kb][step / C::CODE_WORDS]);
     } else if constexpr (C::FP8) {
       const u32x4 u = kr[kb][step / 2];
       f = Tiles<C>::widen(i32x2{static_cast<int>(u[2 * (step % 2)]), static_cast<int>(u[2 * (step % 2) + 1])});
@@ -423,11 +550,14 @@ __device__ __forceinline__ void softmax(Rows<C>& w, Scores<C>& s, Weights<C>& pf
     for (int cb = 0; cb < C::CB; ++cb) {
       const uint32_t seen = static_cast<uint32_t>(w.hi[cb] - w.lo[cb]);
       const int32_t first = j0 + 4 * g - w.lo[cb];
+      const int32_t sinks = C::SINKS ? w.first[cb] - (j0 + 4 * g) : 0;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          s[kb][cb][r] = static_cast<uint32_t>(first + 16 * kb + r) < seen ? s[kb][cb][r] : neg_inf();
+        for (int r = 0; r < 4; ++r) {
+          const bool in = static_cast<uint32_t>(first + 16 * kb + r) < seen || (C::SINKS && 16 * kb + r < sinks);
+          s[kb][cb][r] = in ? s[kb][cb][r] : neg_inf();
+        }
     }
   }
   // the largest score of this lane's keys against the row's bound
@@ -509,6 +639,9 @@ __device__ __forceinline__ void add_infinities(const Tiles<C>& t, Rows<C>& w, in
     if (page < 0 || page >= t.p.num_pages) continue;
     const unsigned char* row =
         t.base_v + page * t.p.v.page + (j & ((1 << t.p.page_shift) - 1)) * static_cast<int64_t>(t.p.v.token);
+    const unsigned char* exps = nullptr;
+    if constexpr (C::FP4)
+      exps = t.base_ve + page * t.p.ve.page + (j & ((1 << t.p.page_shift) - 1)) * static_cast<int64_t>(t.p.ve.token);
 #pragma unroll
     for (int db = 0; db < C::DT / 16; ++db) {
       const int d = 16 * db + 4 * (t.lane >> 4);
@@ -516,12 +649,13 @@ __device__ __forceinline__ void add_infinities(const Tiles<C>& t, Rows<C>& w, in
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         float v;
-        if constexpr (C::FP8) v = (row[d + r] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f;
+        if constexpr (C::FP4) v = exps[d / 32] == 255 ? __builtin_nanf("") : 0.0f;
+        else if constexpr (C::FP8) v = (row[d + r] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f;
         else v = bf16_lo(reinterpret_cast<const uint16_t*>(row)[d + r]);
         if (__builtin_isfinite(v)) continue;
 #pragma unroll
         for (int cb = 0; cb < C::CB; ++cb)
-          if (j >= w.lo[cb] && j < w.hi[cb]) w.o[db][cb][r] += v;
+          if ((j >= w.lo[cb] && j < w.hi[cb]) || (C::SINKS && j < w.first[cb])) w.o[db][cb][r] += v;
       }
     }
   }
@@ -586,7 +720,13 @@ __device__ __forceinline__ bool schedule(const Params& p, int lane, int32_t idx,
       const int32_t span = (C::BM + G - 2) / G + 1, most = p.window < 0x7fffffff - span ? p.window + span : 0x7fffffff;
       keys = keys < most ? keys : most;
     }
-    return Need{(mine.n * G + C::BM - 1) / C::BM, (keys + C::STEP - 1) / C::STEP + (p.window ? 1 : 0)};
+    int32_t steps = (keys + C::STEP - 1) / C::STEP + (p.window ? 1 : 0);
+    if constexpr (C::SINKS) {
+      const int32_t more = (p.sinks < mine.m ? p.sinks + C::STEP - 1 : mine.m + C::STEP - 1) / C::STEP;
+      const int32_t all = (mine.m + C::STEP - 1) / C::STEP;
+      steps = steps < all - more ? steps + more : all;
+    }
+    return Need{(mine.n * G + C::BM - 1) / C::BM, steps};
   };
   const auto parts = [](const Need& x, int32_t per) { return x.steps > per ? (x.steps + per - 1) / per : 1; };
   Need x = need(0);
@@ -699,10 +839,25 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
   const int32_t row_end = row0 + C::BM < R ? row0 + C::BM : R;
   const Range all = range(row0, row_end - 1);
   // key steps of the row tile and of this part
-  const int32_t step0 = all.lo / C::STEP, steps = all.hi > all.lo ? (all.hi + C::STEP - 1) / C::STEP - step0 : 0;
+  const int32_t step0 = all.lo / C::STEP;
+  int32_t steps = all.hi > all.lo ? (all.hi + C::STEP - 1) / C::STEP - step0 : 0;
+  int32_t sink_steps = 0;  // steps of the first keys, before those of the windows and apart from them
+  if constexpr (C::SINKS) {
+    const int32_t upto = p.sinks < all.hi ? (p.sinks + C::STEP - 1) / C::STEP : steps + step0;
+    sink_steps = steps == 0 ? 0 : upto < step0 ? upto : step0;
+    steps += sink_steps;
+  }
   const int32_t first = it.part * it.per;  // one part: 0
   const int32_t rest = steps - first, mine = rest < 0 ? 0 : it.part == it.parts - 1 || rest < it.per ? rest : it.per;
-  const int32_t j_begin = (step0 + first) * C::STEP, count = mine * (C::STEP / C::KT);
+  const int32_t count = mine * (C::STEP / C::KT);
+  // key of this part's tile i
+  const int32_t j_begin = (C::SINKS ? first : step0 + first) * C::STEP;
+  const int32_t apart = sink_steps * C::STEP, skipped = (step0 - sink_steps) * C::STEP;
+  const auto key_of = [&](int32_t i) {
+    const int32_t j = j_begin + i * C::KT;
+    return C::SINKS && j >= apart ? j + skipped : j;
+  };
+  const auto sinks_below = [&](int32_t hi) { return p.sinks < hi ? p.sinks : hi; };
 
   // rows of this wavefront
   const int32_t w0 = row0 + (C::SHARED ? wave * 16 * C::CB : 0);
@@ -723,13 +878,17 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
     const Range x = range(r, r);
     w.lo[cb] = x.lo;
     w.hi[cb] = x.hi;
+    if constexpr (C::SINKS) w.first[cb] = sinks_below(x.hi);
     w.m[cb] = neg_inf();
     w.l[cb] = 0.0f;
     const uint16_t* src = p.q + at_t[cb] * p.ldq + static_cast<int64_t>(at_h[cb]) * p.D;
 #pragma unroll
     for (int step = 0; step < NS; ++step) {
       // the elements that K's operand has there (request_k)
-      const int d = !C::SHARED && C::FP8 ? 64 * (step / 2) + 16 * (lane >> 4) + 8 * (step % 2) : 32 * step + 8 * (lane >> 4);
+      const int d = !C::SHARED && C::FP4   ? 8 * C::LANE_CODES * (step / C::CODE_WORDS) +
+                                                 2 * C::LANE_CODES * (lane >> 4) + 8 * (step % C::CODE_WORDS)
+                    : !C::SHARED && C::FP8 ? 64 * (step / 2) + 16 * (lane >> 4) + 8 * (step % 2)
+                                           : 32 * step + 8 * (lane >> 4);
       u32x4 u = {0u, 0u, 0u, 0u};
       if (d < p.D) u = *reinterpret_cast<const u32x4*>(src + d);
       w.q[step][cb] = __builtin_bit_cast(bf16x8, u);
@@ -744,44 +903,104 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
 
   const float k_scale = p.k.scale ? p.k.scale[head] : 1.0f, v_scale = p.v.scale ? p.v.scale[head] : 1.0f;
   const float c = p.c * k_scale;
-  const auto in_part = [&](int32_t j0) { return j0 < inner.lo || j0 + C::KT > inner.hi; };
+  const auto beyond = [&](int32_t j0, const Range& x) {  // some of the tile's keys are not among x's
+    return (j0 < x.lo || j0 + C::KT > x.hi) && !(C::SINKS && j0 + C::KT <= sinks_below(x.hi));
+  };
+  const auto in_part = [&](int32_t j0) { return beyond(j0, inner); };
   u32x4 kr[C::KT / 16][C::KL];
+  uint32_t ke[C::KT / 16][C::KL];
   Scores<C> sc;
   Weights<C> pf;
-  const auto sees = [&](int32_t j0) { return !C::SHARED || (busy && j0 < any.hi && j0 + C::KT > any.lo); };
-  const auto masked = [&](int32_t j0) { return j0 < full.lo || j0 + C::KT > full.hi; };
+  const auto sees = [&](int32_t j0) {
+    return !C::SHARED || (busy && j0 < any.hi && (j0 + C::KT > any.lo || (C::SINKS && j0 < p.sinks)));
+  };
+  const auto masked = [&](int32_t j0) { return beyond(j0, full); };
 
   if (threadIdx.x == 0) any_infinite = 0;
   __syncthreads();
   if (count > 0) {
-    Tiles<C> t(p, lds + (C::SHARED ? 0 : wave * 2 * C::BUF), lane, wave);
-    t.open(b, head, m, j_begin);
-    if constexpr (C::SHARED) {
-      t.template request<false>(j_begin, 0);
-      t.template request<true>(j_begin, 0);
+    Tiles<C> t(p, lds + (C::SHARED ? 0 : wave * C::BUFFERS * C::BUF), lane, wave);
+    t.open(b, head, m, key_of(0), apart, step0 * C::STEP);
+    if constexpr (C::SHARED && C::FP4) {
+      // codes to registers a tile ahead, from there as bf16 to LDS
+      typename Tiles<C>::Codes ck, cv;
+      const auto fetch = [&](int32_t i) {
+        const int32_t j = key_of(i) + t.first_row(0);
+        t.template fetch<false>(j, ck);
+        t.template fetch<true>(j, cv);
+      };
+      const auto put = [&](int32_t i) {
+        t.template put<false>(ck, t.first_row(0), i & 1, false);
+        const bool some = in_part(key_of(i));
+        if (t.template put<true>(cv, t.first_row(0), i & 1, some) && some) any_infinite = 1;
+      };
+      fetch(0);
+      put(0);
+      if (count > 1) fetch(1);
       for (int32_t i = 0; i < count; ++i) {
-        const int32_t j0 = j_begin + i * C::KT;
-        wait_loads<0>();   // this wavefront's rows of tile i are there,
-        if (in_part(j0) && t.make_finite(i & 1)) any_infinite = 1;
-        group_barrier();   // every wavefront's are, and all have read tile i - 1
+        const int32_t j0 = key_of(i);
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): this wavefront's rows of tile i are written,
+        group_barrier();                     // every wavefront's are, and all have read tile i - 1
         if (i + 1 < count) {
-          t.template request<false>(j0 + C::KT, (i + 1) & 1);
-          t.template request<true>(j0 + C::KT, (i + 1) & 1);
+          put(i + 1);
+          if (i + 2 < count) fetch(i + 2);
         }
         if (sees(j0)) {
-          scores(t, w, kr, i & 1, sc);
+          scores(t, w, kr, ke, i & 1, sc);
           softmax(w, sc, pf, lane, j0, c, masked(j0));
           product(t, w, pf, i & 1);
         }
       }
+    } else if constexpr (C::SHARED) {
+      t.template request<false>(key_of(0), 0);
+      t.template request<true>(key_of(0), 0);
+      for (int32_t i = 0; i < count; ++i) {
+        const int32_t j0 = key_of(i);
+        wait_loads<0>();   // this wavefront's rows of tile i are there,
+        if (in_part(j0) && t.make_finite(i & 1)) any_infinite = 1;
+        group_barrier();   // every wavefront's are, and all have read tile i - 1
+        if (i + 1 < count) {
+          t.template request<false>(key_of(i + 1), (i + 1) & 1);
+          t.template request<true>(key_of(i + 1), (i + 1) & 1);
+        }
+        if (sees(j0)) {
+          scores(t, w, kr, ke, i & 1, sc);
+          softmax(w, sc, pf, lane, j0, c, masked(j0));
+          product(t, w, pf, i & 1);
+        }
+      }
+    } else if constexpr (C::FP4) {
+      typename Tiles<C>::Codes cv[C::KT / 16];
+      const auto fetch = [&](int32_t j) {
+#pragma unroll
+        for (int bl = 0; bl < C::KT / 16; ++bl) t.template fetch<true>(j + 16 * bl, cv[bl]);
+      };
+      if (wave < count) {
+        fetch(key_of(wave));
+        t.request_k4(key_of(wave), kr, ke);
+      }
+      for (int32_t i = wave; i < count; i += C::WAVES) {
+        const int32_t j0 = key_of(i), j1 = key_of(i + C::WAVES);
+        const bool more = i + C::WAVES < count, some = in_part(j0);
+#pragma unroll
+        for (int bl = 0; bl < C::KT / 16; ++bl)
+          if (t.template put<true>(cv[bl], 16 * bl, 0, some) && some) any_infinite = 1;
+        if (more) fetch(j1);
+        scores(t, w, kr, ke, 0, sc);
+        if (more) t.request_k4(j1, kr, ke);  // the registers are free
+        softmax(w, sc, pf, lane, j0, c, masked(j0));
+        product(t, w, pf, 0);
+        asm volatile("" ::: "memory");  // the next rows are written where this tile was read
+        __builtin_amdgcn_sched_barrier(0);
+      }
     } else {
       if (wave < count) {
-        t.template request<true>(j_begin + wave * C::KT, 0);
-        t.request_k(j_begin + wave * C::KT, kr);
+        t.template request<true>(key_of(wave), 0);
+        t.request_k(key_of(wave), kr);
       }
       int at = 0;
       for (int32_t i = wave; i < count; i += C::WAVES, at ^= 1) {
-        const int32_t j0 = j_begin + i * C::KT, j1 = j0 + C::WAVES * C::KT;
+        const int32_t j0 = key_of(i), j1 = key_of(i + C::WAVES);
         const bool more = i + C::WAVES < count;
         if (more) {
           t.template request<true>(j1, at ^ 1);
@@ -790,7 +1009,7 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
           wait_loads<0>();
         }
         if (in_part(j0) && t.make_finite(at)) any_infinite = 1;
-        scores(t, w, kr, at, sc);
+        scores(t, w, kr, ke, at, sc);
         if (more) t.request_k(j1, kr);  // the registers are free
         softmax(w, sc, pf, lane, j0, c, masked(j0));
         product(t, w, pf, at);
@@ -801,7 +1020,7 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
     __syncthreads();
     if (any_infinite) {
       for (int32_t i = C::SHARED ? 0 : wave; i < count; i += C::SHARED ? 1 : C::WAVES)
-        if (in_part(j_begin + i * C::KT)) add_infinities(t, w, j_begin + i * C::KT);
+        if (in_part(key_of(i))) add_infinities(t, w, key_of(i));
     }
   }
 
@@ -892,6 +1111,11 @@ Variant variant(const char* name) {
 // A kernel for sequences of up to `rows` rows, and one for more. dt: 64, 128 or 256.
 __attribute__((visibility("hidden"))) Variant few_rows(int dt, bool fp8, int rows);
 __attribute__((visibility("hidden"))) Variant many_rows(int dt, bool fp8, bool small);
+// The same, with first keys beside the window; over the 4-bit cache (these for all masks).
+__attribute__((visibility("hidden"))) Variant few_rows_sinks(int dt, bool fp8, int rows);
+__attribute__((visibility("hidden"))) Variant many_rows_sinks(int dt, bool fp8, bool small);
+__attribute__((visibility("hidden"))) Variant few_rows4(int dt, int rows);
+__attribute__((visibility("hidden"))) Variant many_rows4(int dt, bool small);
 
 }  // namespace attn
 

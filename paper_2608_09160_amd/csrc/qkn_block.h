@@ -9,6 +9,7 @@
 #include <stdint.h>
 
 #include "qkn_cache.h"
+#include "qkn_cache4.h"
 #include "qkn_host.h"
 
 namespace qkn_block {
@@ -87,6 +88,41 @@ inline bool cache_ok(const qkn_cache& c) {
   if (pool_extent(c, c.k_page, c.k_head, c.k_token) > space || pool_extent(c, c.v_page, c.v_head, c.v_token) > space)
     return false;
   return c.fp8 || (!c.k_scale && !c.v_scale);
+}
+
+// The pools of a 4-bit cache: K's codes, V's, K's exponents, V's.
+struct Pool4 {
+  uint8_t* base;
+  int64_t page, head, token, row;  // strides, and the bytes of a row
+};
+inline Pool4 pool4(const qkn_cache4& c, int i) {
+  const int64_t codes = c.head_dim / 2, exps = c.head_dim / 32;
+  return i == 0   ? Pool4{c.k, c.k_page, c.k_head, c.k_token, codes}
+         : i == 1 ? Pool4{c.v, c.v_page, c.v_head, c.v_token, codes}
+         : i == 2 ? Pool4{c.k_exp, c.ke_page, c.ke_head, c.ke_token, exps}
+                  : Pool4{c.v_exp, c.ve_page, c.ve_head, c.ve_token, exps};
+}
+inline __int128 pool4_extent(const qkn_cache4& c, int i) {
+  if (!c.num_pages) return 0;
+  const Pool4 p = pool4(c, i);
+  return static_cast<__int128>(c.num_pages - 1) * p.page + static_cast<__int128>(c.n_kv - 1) * p.head +
+         static_cast<__int128>(c.page_size - 1) * p.token + p.row;
+}
+inline bool cache4_ok(const qkn_cache4& c) {
+  if (c.num_pages < 0 || c.num_pages > (int64_t{1} << 31) || c.page_size < 1 || c.page_size > 65536 ||
+      (c.page_size & (c.page_size - 1)) || c.n_kv < 1 || c.head_dim < 32 || c.head_dim % 32)
+    return false;
+  for (int i = 0; i < 4; ++i) {
+    const Pool4 p = pool4(c, i);
+    for (int64_t s : {p.page, p.head, p.token})
+      if (s < p.row || s > int64_t{1} << 40) return false;
+    if (pool4_extent(c, i) > int64_t{1} << 46) return false;
+  }
+  return true;
+}
+inline qkn_host::Span pool4_span(const qkn_cache4& c, int i) {
+  const int64_t n = static_cast<int64_t>(pool4_extent(c, i));
+  return qkn_host::Span{reinterpret_cast<uintptr_t>(pool4(c, i).base), n ? 1 : 0, n, n, 1};
 }
 
 // Extent of a pool as one byte region (its gaps included).

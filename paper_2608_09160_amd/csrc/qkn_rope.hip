@@ -21,6 +21,8 @@
 #include <string.h>
 
 #include "qkn_block.h"
+#include "qkn_cache4.h"
+#include "qkn_quant4.h"
 #include "qkn_rope.h"
 
 namespace {
@@ -54,6 +56,7 @@ struct RopeParams {
   const int32_t* pos;
   const int64_t* slots;
   PoolDev kp, vp;
+  PoolDev ke, ve;              // exponents of a 4-bit cache
   int64_t n_slots, n_pos, T;
   int32_t page_shift, page_mask;
   int32_t D, half;             // half: pairs of a head
@@ -124,12 +127,15 @@ __device__ __forceinline__ void store_fp8(uint8_t* p, const float (&f)[V], float
   }
 }
 
+// What the cache holds.
+enum Format { kBf16, kFp8, kFp4 };
+
 // One unit of one token into the cache.
-template <int V, bool FP8>
+template <int V, int F>
 __device__ __forceinline__ void store_cache(const PoolDev& pool, int64_t page, int64_t row, int head, int a, int b,
                                             bool has_b, float scale, const float (&fa)[V], const float (&fb)[V]) {
   const int64_t at = page * pool.page + head * pool.head + row * pool.token;
-  if constexpr (FP8) {
+  if constexpr (F == kFp8) {
     const float rcp = 1.0f / scale;
     uint8_t* p = static_cast<uint8_t*>(pool.base) + at;
     store_fp8<V>(p + a, fa, rcp);
@@ -141,7 +147,38 @@ __device__ __forceinline__ void store_cache(const PoolDev& pool, int64_t page, i
   }
 }
 
-template <int V, bool FP8>
+// One unit into a 4-bit cache: a block's 32 elements are the groups a (and the groups b) of four lanes where pairs are
+// apart, else both groups of two. Units begin at even lanes (of fours where pairs are apart: head and rotated part are
+// multiples of 64 there), so the lanes of a block are neighbours in one wavefront, all of them running.
+__device__ __forceinline__ void store_cache4(const PoolDev& codes, const PoolDev& exps, int64_t page, int64_t row, int head,
+                                             int a, int b, bool apart, bool keep, const float (&fa)[8], const float (&fb)[8]) {
+  uint32_t ma = quant4::magnitude(fa), mb = quant4::magnitude(fb);
+  if (!apart) ma = mb = ma > mb ? ma : mb;
+  ma = quant4::max_of_2(ma);
+  mb = quant4::max_of_2(mb);
+  const uint32_t ma4 = quant4::max_of_4(ma), mb4 = quant4::max_of_4(mb);
+  const uint32_t ea = quant4::exponent(apart ? ma4 : ma), eb = quant4::exponent(apart ? mb4 : mb);
+  const uint32_t ca = quant4::encode(fa, ea), cb = quant4::encode(fb, eb);
+  if (!keep) return;
+  uint8_t* p = static_cast<uint8_t*>(codes.base) + page * codes.page + head * codes.head + row * codes.token;
+  uint8_t* q = static_cast<uint8_t*>(exps.base) + page * exps.page + head * exps.head + row * exps.token;
+  *reinterpret_cast<uint32_t*>(p + a / 2) = ca;
+  *reinterpret_cast<uint32_t*>(p + b / 2) = cb;
+  if (a % 32 == 0) q[a / 32] = static_cast<uint8_t>(ea);
+  if (b % 32 == 0) q[b / 32] = static_cast<uint8_t>(eb);
+}
+
+// x c + y s. APART: each operation rounded by itself, as what the 4-bit quantiser gets must not depend on the path.
+template <bool APART>
+__device__ __forceinline__ float cross(float x, float c, float y, float s) {
+  if constexpr (APART) {
+    return quant4::cross(x, c, y, s);
+  } else {
+    return x * c + y * s;
+  }
+}
+
+template <int V, int F>
 __global__ __launch_bounds__(64 * kWaves) void qkn_rope(const RopeParams p) {
   const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + (threadIdx.x >> 6));
   const uint32_t t32 = div(wave, p.parts);
@@ -174,7 +211,7 @@ __global__ __launch_bounds__(64 * kWaves) void qkn_rope(const RopeParams p) {
   if (p.half) at = p.pos[t];
   if (p.cached) {
     slot = p.slots[t];
-    if constexpr (FP8) {
+    if constexpr (F == kFp8) {
       const float* sc = of_v ? p.vp.scale : p.kp.scale;
       if (sc && !of_q) scale = sc[head];
     }
@@ -226,18 +263,18 @@ __global__ __launch_bounds__(64 * kWaves) void qkn_rope(const RopeParams p) {
         for (int e = 0; e < V; e += 2) {
           const float c0 = cs[e / 2][0], s0 = cs[e / 2][1], c1 = cs[V / 2 + e / 2][0], s1 = cs[V / 2 + e / 2][1];
           const float x0 = fa[e], x1 = fa[e + 1], y0 = fb[e], y1 = fb[e + 1];
-          fa[e] = x0 * c0 - x1 * s0;
-          fa[e + 1] = x1 * c0 + x0 * s0;
-          fb[e] = y0 * c1 - y1 * s1;
-          fb[e + 1] = y1 * c1 + y0 * s1;
+          fa[e] = cross<F == kFp4>(x0, c0, -x1, s0);
+          fa[e + 1] = cross<F == kFp4>(x1, c0, x0, s0);
+          fb[e] = cross<F == kFp4>(y0, c1, -y1, s1);
+          fb[e + 1] = cross<F == kFp4>(y1, c1, y0, s1);
         }
       }
     } else {
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float xa = fa[e], xb = fb[e];
-        fa[e] = xa * cs[e][0] - xb * cs[e][1];
-        fb[e] = xb * cs[e][0] + xa * cs[e][1];
+        fa[e] = cross<F == kFp4>(xa, cs[e][0], -xb, cs[e][1]);
+        fb[e] = cross<F == kFp4>(xb, cs[e][0], xa, cs[e][1]);
       }
     }
   }
@@ -248,13 +285,78 @@ __global__ __launch_bounds__(64 * kWaves) void qkn_rope(const RopeParams p) {
     store_bf16<V>(y + a, fa);
     if (has_b) store_bf16<V>(y + b, fb);
   }
-  if (p.cached && !of_q) {
-    if (slot >= 0 && slot < p.n_slots) {
-      const int64_t page = slot >> p.page_shift, row = slot & p.page_mask;
-      if (of_v) store_cache<V, FP8>(p.vp, page, row, head, a, b, has_b, scale, fa, fb);
-      else store_cache<V, FP8>(p.kp, page, row, head, a, b, has_b, scale, fa, fb);
+  const bool keep = !of_q && slot >= 0 && slot < p.n_slots;
+  const int64_t page = slot >> p.page_shift, row = slot & p.page_mask;
+  if constexpr (F == kFp4) {
+    if constexpr (V == 8)
+      if (p.cached) store_cache4(of_v ? p.vp : p.kp, of_v ? p.ve : p.ke, page, row, head, a, b, apart, keep, fa, fb);
+  } else if (p.cached && keep) {
+    if (of_v) store_cache<V, F>(p.vp, page, row, head, a, b, has_b, scale, fa, fb);
+    else store_cache<V, F>(p.kp, page, row, head, a, b, has_b, scale, fa, fb);
+  }
+}
+
+// K and V into a 4-bit cache where rows do not fit the vectors: half a wavefront for 32 elements, a lane each.
+struct Elements4 {
+  FastDiv blocks, per_head;  // blocks of a token (K's and V's); of a head
+  int32_t k_blocks;
+};
+__global__ __launch_bounds__(64 * kWaves) void qkn_rope4_elements(const RopeParams p, const Elements4 x) {
+  const uint32_t block = blockIdx.x * (2 * kWaves) + (threadIdx.x >> 5);
+  const uint32_t t32 = div(block, x.blocks);
+  const int64_t t = t32;
+  if (t >= p.T) return;  // half a wavefront at a time
+  const int lane = static_cast<int>(threadIdx.x) & 31, in_token = static_cast<int>(block - t32 * x.blocks.d);
+  const bool of_v = in_token >= x.k_blocks;
+  const int in_seg = in_token - (of_v ? x.k_blocks : 0);
+  const int head = static_cast<int>(div(static_cast<uint32_t>(in_seg), x.per_head));
+  const int c = 32 * (in_seg - head * static_cast<int>(x.per_head.d)) + lane;
+
+  const uint16_t* row_x = (of_v ? p.v + t * p.ldv : p.k.x + t * p.k.ldx) + head * p.D;
+  float f = bf16_lo(row_x[c]);
+  if (!of_v) {
+    const bool turns = c < 2 * p.half;
+    const bool second = turns && (p.interleaved ? (c & 1) != 0 : c >= p.half);
+    const int pair = p.interleaved ? c / 2 : second ? c - p.half : c;
+    const int other = !turns ? c : p.interleaved ? (c ^ 1) : second ? c - p.half : c + p.half;
+    float g = bf16_lo(row_x[other]);
+    if (p.k.w) {
+      float ranks[kRanks];
+      load_ranks(p.k.partials, t, p.T, p.tp, 0, ranks);
+      const float inv = __builtin_amdgcn_rsqf(__builtin_fmaf(rank_sum(p.k.partials, t, p.T, p.tp, ranks), p.k.rcp_d, p.eps));
+      const float* w = p.k.w + head * p.D;
+      f = f * w[c] * inv;
+      g = g * w[other] * inv;
+    }
+    if (turns) {
+      const int32_t at = p.pos[t];
+      if (at >= 0 && at < p.n_pos) {
+        const float* cs = p.table + 2 * (static_cast<int64_t>(at) * p.half + pair);
+        f = quant4::cross(f, cs[0], second ? g : -g, cs[1]);
+      } else {
+        f = __builtin_nanf("");
+      }
     }
   }
+  uint32_t most = __builtin_bit_cast(uint32_t, f) & 0x7fffffffu;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const uint32_t m = static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), d));
+    most = m > most ? m : most;
+  }
+  const uint32_t e = quant4::exponent(most);
+  const float next = __shfl_xor(f, 1);
+  const int64_t slot = p.slots[t];
+  if (slot < 0 || slot >= p.n_slots) return;
+  const int64_t page = slot >> p.page_shift, row = slot & p.page_mask;
+  const PoolDev& codes = of_v ? p.vp : p.kp;
+  const PoolDev& exps = of_v ? p.ve : p.ke;
+  if (lane % 2 == 0)
+    (static_cast<uint8_t*>(codes.base) + page * codes.page + head * codes.head + row * codes.token)[c / 2] =
+        static_cast<uint8_t>(quant4::encode2(f, next, e));
+  if (lane == 0)
+    (static_cast<uint8_t*>(exps.base) + page * exps.page + head * exps.head + row * exps.token)[c / 32] =
+        static_cast<uint8_t>(e);
 }
 
 // Frequencies and angles in 64 bits: an angle of 10^6 radians in 32 bits is off by up to 0.03.
@@ -296,9 +398,11 @@ bool vec_rows(const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 == 0;
 
 int rope_impl(const qkn_rope_seg* q, const qkn_rope_seg* k, const uint16_t* v, int64_t ldv, int64_t T, int head_dim,
               int rot_dim, int interleaved, const float* table, int64_t n_pos, const int32_t* pos,
-              const int64_t* slots, const qkn_cache* cache, int tp, float eps, void* stream) {
+              const int64_t* slots, const qkn_cache* cache, const qkn_cache4* cache4, int tp, float eps, void* stream) {
+  const bool cached = cache || cache4;
+  const int32_t n_kv = cache ? cache->n_kv : cache4 ? cache4->n_kv : 0;
   if ((!q && !k) || head_dim < 1 || rot_dim < 0 || rot_dim > head_dim || rot_dim % 2 || T < 0 || tp < 1 ||
-      !(eps >= 0.0f) || isinf(eps) || (v && !cache) || (rot_dim && n_pos < 0))
+      !(eps >= 0.0f) || isinf(eps) || (v && !cached) || (rot_dim && n_pos < 0))
     return QKN_EINVAL;
   const int64_t D = head_dim, most = int64_t{1} << 30;
   int64_t units[3] = {0, 0, 0};
@@ -311,17 +415,21 @@ int rope_impl(const qkn_rope_seg* q, const qkn_rope_seg* k, const uint16_t* v, i
     if (s->ldx < width || (s->y && s->ldy < width) || (s->w && s->d_full < width)) return QKN_EINVAL;
     if (width > most) return QKN_ENOTSUP;
   }
-  if (k && !k->y && !cache) return QKN_EINVAL;
+  if (k && !k->y && !cached) return QKN_EINVAL;
   if (cache && (!cache_ok(*cache) || cache->head_dim != head_dim || (k && k->heads != cache->n_kv) || (!k && !v)))
     return QKN_EINVAL;
-  if (v && (ldv < cache->n_kv * D)) return QKN_EINVAL;
-  if (v && cache->n_kv * D > most) return QKN_ENOTSUP;
+  if (cache4 && (!cache4_ok(*cache4) || cache4->head_dim != head_dim || (k && k->heads != n_kv) || (!k && !v)))
+    return QKN_EINVAL;
+  if (v && ldv < n_kv * D) return QKN_EINVAL;
+  if (v && n_kv * D > most) return QKN_ENOTSUP;
   if (T == 0) return QKN_OK;
   for (const qkn_rope_seg* s : segs)
     if (s && (!s->x || (s->w && !s->partials))) return QKN_EINVAL;
   if (q && !q->y) return QKN_EINVAL;
   if (rot_dim && (!table || !pos)) return QKN_EINVAL;
   if (cache && (!slots || (cache->num_pages && ((k && !cache->k) || (v && !cache->v))))) return QKN_EINVAL;
+  if (cache4 && (!slots || (cache4->num_pages && ((k && (!cache4->k || !cache4->k_exp)) || (v && (!cache4->v || !cache4->v_exp))))))
+    return QKN_EINVAL;
 
   Regions r;
   bool vec = D % 16 == 0 && rot_dim % 16 == 0;
@@ -340,7 +448,7 @@ int rope_impl(const qkn_rope_seg* q, const qkn_rope_seg* k, const uint16_t* v, i
     }
   }
   if (v) {
-    r.add(Span{reinterpret_cast<uintptr_t>(v), T, ldv, cache->n_kv * D, 2}, false);
+    r.add(Span{reinterpret_cast<uintptr_t>(v), T, ldv, n_kv * D, 2}, false);
     vec = vec && vec_rows(v, ldv);
   }
   if (rot_dim) {
@@ -364,18 +472,42 @@ int rope_impl(const qkn_rope_seg* q, const qkn_rope_seg* k, const uint16_t* v, i
     }
     if (k && v && c.num_pages && c.k == c.v) return QKN_EOVERLAP;
   }
-  const bool two_pools = cache && k && v;  // they may share an allocation, their rows in turn
+  int pools = cache && k && v ? 2 : 0;  // at the end of the list: they may share an allocation, their rows in turn
+  bool fit4 = true;
+  if (cache4) {
+    r.add(array_span(slots, T, 8), false);
+    for (int i = 0; i < 4; ++i) {
+      if (!(i % 2 ? v != nullptr : k != nullptr)) continue;
+      for (int j = 0; j < i; ++j)
+        if ((j % 2 ? v != nullptr : k != nullptr) && cache4->num_pages && pool4(*cache4, i).base == pool4(*cache4, j).base)
+          return QKN_EOVERLAP;
+      r.add(pool4_span(*cache4, i), true);
+      ++pools;
+      const Pool4 x = pool4(*cache4, i);
+      if (i < 2) fit4 = fit4 && aligned(x.base, 4) && x.page % 4 == 0 && x.head % 4 == 0 && x.token % 4 == 0;
+    }
+    // a block's elements on neighbouring lanes
+    fit4 = fit4 && rot_dim % 32 == 0 && (interleaved || rot_dim == 0 || (D % 64 == 0 && rot_dim % 64 == 0));
+  }
   for (int a = 0; a < r.n; ++a)
     for (int b = a + 1; b < r.n; ++b) {
-      if (two_pools && a == r.n - 2 && b == r.n - 1) continue;
+      if (a >= r.n - pools) continue;
       if ((r.out[a] || r.out[b]) && spans_overlap(r.item[a], r.item[b])) return QKN_EOVERLAP;
     }
 
   const int64_t V = vec ? 8 : 1, per_head = (D + 2 * V - 1) / (2 * V);
   if (q) units[0] = q->heads * per_head;
   if (k) units[1] = k->heads * per_head;
-  if (v) units[2] = cache->n_kv * per_head;
-  const int64_t all = units[0] + units[1] + units[2], parts = (all + 63) / 64;
+  if (v) units[2] = n_kv * per_head;
+  // K and V of a 4-bit cache that do not fit the vectors go by themselves, before K's rows may be written in place
+  const bool elements = cache4 && !(vec && fit4);
+  const int64_t blocks = elements ? ((k ? n_kv : 0) + (v ? n_kv : 0)) * (D / 32) : 0;
+  if (elements) {
+    if (T * blocks > (int64_t{1} << 31) - 8) return QKN_ENOTSUP;
+    units[2] = 0;
+    if (k && !k->y) units[1] = 0;
+  }
+  const int64_t all = units[0] + units[1] + units[2], parts = all ? (all + 63) / 64 : 1;
   if (all > most || T > (int64_t{1} << 31) - 8 || T * parts > (int64_t{1} << 31) - 8) return QKN_ENOTSUP;
 
   RopeParams p;
@@ -410,20 +542,47 @@ int rope_impl(const qkn_rope_seg* q, const qkn_rope_seg* k, const uint16_t* v, i
   p.per_head = fast_div(static_cast<uint32_t>(per_head));
   p.parts = fast_div(static_cast<uint32_t>(parts));
 
-  const bool fp8 = cache && cache->fp8;
+  if (cache4) {
+    const qkn_cache4& c = *cache4;
+    const auto dev = [&](int i) {
+      const Pool4 x = pool4(c, i);
+      return PoolDev{x.base, nullptr, x.page, x.head, x.token};
+    };
+    p.kp = dev(0);
+    p.vp = dev(1);
+    p.ke = dev(2);
+    p.ve = dev(3);
+    p.n_slots = c.num_pages * c.page_size;
+    p.page_shift = log2_of(c.page_size);
+    p.page_mask = c.page_size - 1;
+    p.cached = 1;
+  }
+
+  const Format f = cache4 ? kFp4 : cache && cache->fp8 ? kFp8 : kBf16;
   const int64_t grid = (T * parts + kWaves - 1) / kWaves;
-  const char* name = vec ? (fp8 ? "rope<8>/fp8" : "rope<8>/bf16") : (fp8 ? "rope<1>/fp8" : "rope<1>/bf16");
+  const char* name = elements ? "rope4/elements" : f == kFp4 ? "rope<8>/fp4"
+                     : vec    ? (f == kFp8 ? "rope<8>/fp8" : "rope<8>/bf16")
+                              : (f == kFp8 ? "rope<1>/fp8" : "rope<1>/bf16");
   if (qkn_host::validate_only()) {
     qkn_host::record_launch(qkn_launch_info{name, 0, 0, 0, 0});
     return QKN_EDRYRUN;
   }
-  const void* fn = vec ? (fp8 ? reinterpret_cast<const void*>(qkn_rope<8, true>)
-                              : reinterpret_cast<const void*>(qkn_rope<8, false>))
-                       : (fp8 ? reinterpret_cast<const void*>(qkn_rope<1, true>)
-                              : reinterpret_cast<const void*>(qkn_rope<1, false>));
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  if (elements) {
+    Elements4 x{fast_div(static_cast<uint32_t>(blocks)), fast_div(static_cast<uint32_t>(D / 32)),
+                static_cast<int32_t>(k ? n_kv * (D / 32) : 0)};
+    void* args[] = {&p, &x};
+    if (hipLaunchKernel(reinterpret_cast<const void*>(qkn_rope4_elements),
+                        dim3(static_cast<unsigned>((T * blocks + 2 * kWaves - 1) / (2 * kWaves))), dim3(64 * kWaves), args, 0,
+                        st) != hipSuccess)
+      return QKN_EHIP;
+    p.cached = 0;  // the rest writes rows only
+  }
+  const auto kernel = vec ? (f == kFp4 ? qkn_rope<8, kFp4> : f == kFp8 ? qkn_rope<8, kFp8> : qkn_rope<8, kBf16>)
+                          : (f == kFp4 ? qkn_rope<1, kFp4> : f == kFp8 ? qkn_rope<1, kFp8> : qkn_rope<1, kBf16>);
+  const void* fn = reinterpret_cast<const void*>(kernel);
   void* args[] = {&p};
-  if (hipLaunchKernel(fn, dim3(static_cast<unsigned>(grid)), dim3(64 * kWaves), args, 0,
-                      static_cast<hipStream_t>(stream)) != hipSuccess)
+  if (all && hipLaunchKernel(fn, dim3(static_cast<unsigned>(grid)), dim3(64 * kWaves), args, 0, st) != hipSuccess)
     return QKN_EHIP;
   qkn_host::record_launch(qkn_launch_info{name, grid, 64 * kWaves, grid * kWaves, 0});
   return QKN_OK;
@@ -464,7 +623,14 @@ int qkn_rope_table(float* table, int64_t n_pos, int rot_dim, const qkn_rope_scal
 int qkn_rope_cache(const qkn_rope_seg* q, const qkn_rope_seg* k, const uint16_t* v, int64_t ldv, int64_t T,
                    int head_dim, int rot_dim, int interleaved, const float* table, int64_t n_pos, const int32_t* pos,
                    const int64_t* slots, const qkn_cache* cache, int tp, float eps, void* stream) {
-  return rope_impl(q, k, v, ldv, T, head_dim, rot_dim, interleaved, table, n_pos, pos, slots, cache, tp, eps, stream);
+  return rope_impl(q, k, v, ldv, T, head_dim, rot_dim, interleaved, table, n_pos, pos, slots, cache, nullptr, tp, eps, stream);
+}
+
+int qkn_rope_cache4(const qkn_rope_seg* q, const qkn_rope_seg* k, const uint16_t* v, int64_t ldv, int64_t T,
+                    int head_dim, int rot_dim, int interleaved, const float* table, int64_t n_pos, const int32_t* pos,
+                    const int64_t* slots, const qkn_cache4* cache, int tp, float eps, void* stream) {
+  if (!cache) return QKN_EINVAL;
+  return rope_impl(q, k, v, ldv, T, head_dim, rot_dim, interleaved, table, n_pos, pos, slots, nullptr, cache, tp, eps, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,257 @@
+"""The 4-bit cache: its format, the write behind the rotary positions, rows read back, against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_09160_amd as qkn
+from oracle import block as B
+from oracle import cache4 as O
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+ULP = 2.0 ** -24
+
+
+def _host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _bytes(t):
+    return t.cpu().numpy()
+
+
+def _rows(g, T, width, pad=0, shift=0):
+    """bf16 rows inside a wider buffer: stride width + pad, first element `shift` elements in."""
+    buf = torch.randn(T * (width + pad) + shift, generator=g).to(torch.bfloat16).to(DEV)
+    return buf[shift:].view(T, width + pad)[:, :width]
+
+
+def _cache(g, pages, heads, page, D, order="heads first", pad=0):
+    """Pools of random bytes; `pad` bytes between rows of the codes."""
+    def pool(width, pad=0):
+        shape = (pages, page, heads) if order == "rows first" else (pages, heads, page)
+        x = torch.randint(0, 256, (*shape, width + pad), dtype=torch.uint8, generator=g).to(DEV)[..., :width]
+        return x.transpose(1, 2) if order == "rows first" else x
+    return qkn.KVCache4(pool(D // 2, pad), pool(D // 2, pad), pool(D // 32), pool(D // 32))
+
+
+def _at(pool, slots, page):
+    """Rows `slots` of a pool: [T, heads, width]."""
+    return _bytes(pool)[slots // page, :, slots % page]
+
+
+def test_every_code_under_every_exponent():
+    codes = torch.arange(256, dtype=torch.uint8).repeat(256, 1, 1, 1).to(DEV)
+    exps = torch.arange(256, dtype=torch.uint8).view(256, 1, 1, 1).repeat(1, 1, 1, 16).to(DEV)
+    k, v = qkn.qkn_cache4_load(qkn.KVCache4(codes, codes.clone(), exps, exps.clone()), torch.arange(256, device=DEV))
+    ref = O.values(_bytes(codes)[:, 0, 0], _bytes(exps)[:, 0, 0])
+    for got in (k, v):
+        assert np.array_equal(_host(got)[2:253], ref[2:253])
+        assert got[255].isnan().all()
+
+
+@pytest.mark.parametrize("D,pad,shift,kernel", [(128, 0, 0, "rope<8>/fp4"), (32, 0, 0, "rope<8>/fp4"), (96, 0, 0, "rope<8>/fp4"),
+                                                (64, 3, 1, "rope4/elements")])
+def test_quantiser(D, pad, shift, kernel):
+    """Rows as they are: codes and exponents are the definition's, each one of them."""
+    g = torch.Generator().manual_seed(D)
+    T = 3000
+    x = _rows(g, T, 2 * D, pad, shift)
+    x *= torch.exp2(torch.randint(-30, 30, (T, 1), generator=g).float()).to(DEV)
+    ties = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.5, 6.0, 7.0, -0.25, -0.75, -5.0, -0.0, 0.0, 6.9]
+    x[0, :16] = torch.tensor(ties)
+    x[1, :16] = torch.tensor(ties) * 2.0 ** 90
+    x[1, 9] = 0
+    x[2] = 0
+    x[3] = -0.0
+    x[4, 5] = float("inf")
+    x[5, 2] = -float("inf")
+    x[6, 7] = float("nan")
+    x[7] = 3.3e38
+    x[8] = 1e-38
+    x[9, :32] = 2.0 ** -133
+    x[10, :8] = torch.tensor([7.0, 6.97, 1.75, 1.745, 3.5, 0.109, 0.1, 14.0])
+    cache = _cache(g, T // 16 + 1, 2, 16, D)
+    slots = torch.randperm(T // 16 * 16 + 16, generator=g)[:T].to(DEV)
+    qkn.qkn_rope_cache(None, None, D, k=qkn.RopeSeg(x), v=x, cache=cache, slots=slots)
+    assert qkn.qkn_last_launch()["kernel"] == kernel
+    codes, exps = O.quantised(_host(x).reshape(T, 2, D))
+    at = slots.cpu().numpy()
+    for pool, want in ((cache.k, codes), (cache.v, codes), (cache.k_exp, exps), (cache.v_exp, exps)):
+        assert np.array_equal(_at(pool, at, 16), want)
+    k, v = qkn.qkn_cache4_load(cache, slots)
+    ref = O.values(codes, exps).reshape(T, -1)
+    assert np.array_equal(_host(k), ref, equal_nan=True) and np.array_equal(_host(v), ref, equal_nan=True)
+
+
+CASES = [
+    # T, heads, kv heads, D, rot, interleaved, tp (0: no norm), page, row pad, row shift, pool order, pool pad, elements
+    (1, 1, 1, 32, 32, False, 1, 1, 0, 0, "heads first", 0, True),
+    (3, 8, 2, 128, 128, False, 4, 16, 0, 0, "heads first", 0, False),
+    (70, 5, 1, 128, 64, False, 8, 32, 8, 0, "rows first", 0, False),
+    (33, 4, 4, 64, 64, True, 2, 16, 16, 8, "heads first", 16, False),
+    (129, 6, 2, 96, 32, True, 0, 64, 0, 0, "rows first", 0, False),
+    (129, 6, 2, 96, 32, False, 0, 64, 0, 0, "rows first", 0, True),
+    (17, 3, 1, 256, 256, False, 3, 8, 0, 0, "heads first", 0, False),
+    (17, 3, 1, 256, 128, False, 3, 8, 0, 0, "heads first", 3, True),     # code rows not aligned to words
+    (9, 7, 7, 32, 0, False, 5, 16, 0, 0, "heads first", 0, False),       # no rotation
+    (9, 7, 7, 32, 16, False, 5, 16, 0, 0, "heads first", 0, True),
+    (21, 3, 1, 160, 26, True, 2, 16, 1, 1, "rows first", 0, True),
+    (12, 2, 2, 64, 24, False, 2, 4, 0, 0, "heads first", 0, True),       # half a vector rotates
+    (40, 4, 2, 128, 128, False, 2, 16, 0, 1, "heads first", 0, True),    # rows not aligned to 16 bytes
+    (2100, 16, 2, 128, 128, False, 4, 64, 0, 0, "heads first", 0, False),
+]
+
+
+@pytest.mark.parametrize("T,hq,hk,D,rot,inter,tp,page,pad,shift,order,gap,elements", CASES)
+def test_write_against_the_definition(T, hq, hk, D, rot, inter, tp, page, pad, shift, order, gap, elements):
+    g = torch.Generator().manual_seed(T * 1000 + D + rot)
+    n_pos = 5000
+    q, k, v = (_rows(g, T, h * D, pad, shift) for h in (hq, hk, hk))
+    table = qkn.qkn_rope_table(n_pos, rot, base=500.0) if rot else None
+    pos = torch.randint(0, n_pos, (T,), generator=g).int().to(DEV)
+    pages = (T + page - 1) // page + 2
+    cache = _cache(g, pages, hk, page, D, order, gap)
+    slots = torch.randperm(pages * page, generator=g)[:T]
+    if T > 2:
+        slots[1] = -1  # a padding token
+        slots[2] = pages * page  # beyond the cache
+    pools = (cache.k, cache.v, cache.k_exp, cache.v_exp)
+    before = [_bytes(p).copy() for p in pools]
+    segs, z = [], []
+    for x, h in ((q, hq), (k, hk)):
+        ref = _host(x)
+        if tp:
+            w = (torch.rand(h * D, generator=g) + 0.5).to(DEV)
+            P = (torch.rand(tp, T, generator=g) * h * D + 1).to(DEV)
+            ref = B.normed(ref, _host(w), _host(P), h * D * tp, 1e-6)
+            segs.append(qkn.RopeSeg(x=x, w=w, partials=P, d_full=h * D * tp))
+        else:
+            segs.append(qkn.RopeSeg(x=x))
+        z.append(ref)
+    segs[1].y = torch.empty(T, hk * D, dtype=torch.bfloat16, device=DEV)
+    yq = qkn.qkn_rope_cache(table, pos, D, q=segs[0], k=segs[1], v=v, cache=cache, slots=slots.to(DEV), interleaved=inter)
+    assert qkn.qkn_last_launch()["kernel"] == ("rope4/elements" if elements else "rope<8>/fp4")
+    torch.cuda.synchronize()
+
+    # fp32 rounding: the ranks' sum, mean, root and two products of the norm (tp + 6), the rotation's products, sum
+    # and table entries (6)
+    unit = (max(tp, 1) + 12) * ULP
+    exact = B.rope_table(n_pos, rot, base=500.0) if rot else None
+    for name, zz, y in (("q", z[0], yq), ("k", z[1], segs[1].y)):
+        ref, size = B.rotated(zz, exact, pos.cpu().numpy(), D, rot, inter)
+        B.check_rounded(_host(y), ref, unit * size, "bf16", name)
+    sl = slots.numpy()
+    kept = (sl >= 0) & (sl < pages * page)
+    at = sl[kept]
+    O.check_stored(_at(cache.k, at, page), _at(cache.k_exp, at, page), ref.reshape(T, hk, D)[kept],
+                   unit * size.reshape(T, hk, D)[kept], "k")
+    codes, exps = O.quantised(_host(v).reshape(T, hk, D)[kept])
+    assert np.array_equal(_at(cache.v, at, page), codes) and np.array_equal(_at(cache.v_exp, at, page), exps)
+    for pool, want in zip(pools, before):
+        got = _bytes(pool).copy()
+        want[at // page, :, at % page] = got[at // page, :, at % page]
+        assert np.array_equal(got, want), "rows that no slot names were written"
+    # read back, padding tokens as zeros, into rows of another stride
+    for gap in (0, 8, 3):
+        wide = [torch.full((T, hk * D + gap), 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+        rows = [w[:, :hk * D] for w in wide]
+        qkn.qkn_cache4_load(cache, slots.to(DEV), *rows)
+        for got, c, e in zip(rows, (cache.k, cache.v), (cache.k_exp, cache.v_exp)):
+            ref4 = np.zeros((T, hk * D))
+            ref4[kept] = O.values(_at(c, at, page), _at(e, at, page)).reshape(len(at), -1)
+            assert np.array_equal(_host(got), ref4)
+        assert all((w[:, hk * D:] == 7).all() for w in wide)
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("tp", [0, 1, 6])
+def test_codes_do_not_depend_on_the_path(tp, inter):
+    """The same rows by vectors and element by element: the same bytes; in place too, and K or V alone."""
+    g = torch.Generator().manual_seed(tp)
+    T, hk, D, page = 700, 3, 128, 16
+    k, v = (_rows(g, T, hk * D) for _ in range(2))
+    table, pos = qkn.qkn_rope_table(T, D), torch.arange(T, dtype=torch.int32, device=DEV)
+    more = {}
+    if tp:
+        more = dict(w=torch.rand(hk * D, generator=g).to(DEV) + 0.5, d_full=hk * D * tp,
+                    partials=(torch.rand(tp, T, generator=g) * hk * D + 1).to(DEV))
+    slots = torch.randperm(T // page * page + page, generator=g)[:T].to(DEV)
+    caches = [qkn.KVCache4.empty(T // page + 1, hk, page, D, DEV) for _ in range(4)]
+    for c in caches:
+        for p in (c.k, c.v, c.k_exp, c.v_exp):
+            p.zero_()
+    call = dict(slots=slots, interleaved=inter)
+    qkn.qkn_rope_cache(table, pos, D, k=qkn.RopeSeg(k, **more), v=v, cache=caches[0], **call)
+    assert qkn.qkn_last_launch()["kernel"] == "rope<8>/fp4"
+    odd = [torch.empty(T * (hk * D + 1) + 1, dtype=torch.bfloat16, device=DEV)[1:].view(T, -1)[:, :-1].copy_(x) for x in (k, v)]
+    y = torch.empty_like(odd[0])
+    qkn.qkn_rope_cache(table, pos, D, k=qkn.RopeSeg(odd[0], y=odd[0], **more), v=odd[1], cache=caches[1], **call)
+    assert qkn.qkn_last_launch()["kernel"] == "rope4/elements"
+    qkn.qkn_rope_cache(table, pos, D, k=qkn.RopeSeg(k, y=y, **more), cache=caches[2], **call)
+    qkn.qkn_rope_cache(table, pos, D, q=qkn.RopeSeg(k, y=torch.empty_like(k), **more), v=v, cache=caches[2], **call)
+    z = k.clone()
+    qkn.qkn_rope_cache(table, pos, D, q=qkn.RopeSeg(k, y=torch.empty_like(k), **more), k=qkn.RopeSeg(z, y=z, **more), v=v,
+                       cache=caches[3], **call)
+    for c in caches[1:]:
+        for name in ("k", "v", "k_exp", "v_exp"):
+            assert torch.equal(getattr(c, name), getattr(caches[0], name)), name
+    # rows in place are the other call's, whichever path
+    assert torch.equal(odd[0], z) and torch.equal(y, z)
+
+
+def test_positions_outside_the_table_make_the_rotated_blocks_nan():
+    D = 128
+    x = torch.ones(3, D, dtype=torch.bfloat16, device=DEV)
+    for shift in (0, 1):
+        rows = torch.ones(3 * D + 1, dtype=torch.bfloat16, device=DEV)[shift:shift + 3 * D].view(3, D)
+        cache = qkn.KVCache4.empty(1, 1, 16, D, DEV)
+        pos = torch.tensor([-1, 8, 0], dtype=torch.int32, device=DEV)
+        qkn.qkn_rope_cache(qkn.qkn_rope_table(8, 64), pos, D, k=qkn.RopeSeg(rows), v=x, cache=cache,
+                           slots=torch.arange(3, device=DEV))
+        assert cache.k_exp[0, 0, :3].tolist() == [[255, 255, 125, 125], [255, 255, 125, 125], [125] * 4]
+        k, v = qkn.qkn_cache4_load(cache, torch.arange(3, device=DEV))
+        assert k[:2, :64].isnan().all() and (k[:2, 64:] == 1).all() and (k[2] == 1).all() and (v == 1).all()
+
+
+def test_graph_other_stream_and_one_allocation():
+    g = torch.Generator().manual_seed(6)
+    T, D, hk, page = 50, 64, 2, 16
+    both = torch.zeros(6, 2, hk, page, D // 2 + 16, dtype=torch.uint8, device=DEV)  # codes, then exponents, K and V in turn
+    cache = qkn.KVCache4(both[:, 0, ..., :D // 2], both[:, 1, ..., :D // 2], both[:, 0, ..., D // 2:D // 2 + 2],
+                         both[:, 1, ..., D // 2:D // 2 + 2])
+    q, k, v = (_rows(g, T, h * D) for h in (4, hk, hk))
+    table, pos = qkn.qkn_rope_table(T, D), torch.arange(T, dtype=torch.int32, device=DEV)
+    slots = torch.arange(T, device=DEV) + 3
+    write = qkn.PreparedRopeCache(table, pos, D, q=qkn.RopeSeg(q), k=qkn.RopeSeg(k), v=v, cache=cache, slots=slots)
+    read = qkn.PreparedCache4Load(cache, slots)
+    write()
+    read()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (both, write.q.y, read.k, read.v)]
+    assert (want[0][..., D // 2 + 2:] == 0).all()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        write()
+        read()
+    for _ in range(3):
+        for t in (both, write.q.y, read.k, read.v):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, w) for t, w in zip((both, write.q.y, read.k, read.v), want))
+
+
+def test_no_tokens_and_no_pages():
+    none = torch.empty(0, dtype=torch.int64, device=DEV)
+    cache = qkn.KVCache4.empty(2, 1, 16, 64, DEV)
+    x = torch.empty(0, 64, dtype=torch.bfloat16, device=DEV)
+    qkn.qkn_rope_cache(None, None, 64, k=qkn.RopeSeg(x), v=x, cache=cache, slots=none)
+    k, v = qkn.qkn_cache4_load(cache, none)
+    assert k.shape == v.shape == (0, 64)
+    cache = qkn.KVCache4.empty(0, 1, 16, 64, DEV)
+    x = torch.ones(2, 64, dtype=torch.bfloat16, device=DEV)
+    slots = torch.zeros(2, dtype=torch.int64, device=DEV)
+    qkn.qkn_rope_cache(None, None, 64, k=qkn.RopeSeg(x), v=x, cache=cache, slots=slots)
+    assert all(t.count_nonzero() == 0 for t in qkn.qkn_cache4_load(cache, slots))
