@@ -18,3 +18,6 @@ from ._lib import (QKN_EHIP, QKN_EINVAL, QKN_ENOTSUP, QKN_EOVERLAP, QKN_OK,  # n
 from ._serve import (AdapterSeg, KVCache, KVCache4, PreparedAdapters, PreparedAttn, PreparedCache4Load,  # noqa: F401
                      PreparedRopeCache, RopeSeg, qkn_adapters_add, qkn_attn, qkn_cache4_load, qkn_rope_cache,
                      qkn_rope_table)
+from ._pages import (PageBook, PreparedPagesCompact, PreparedPagesCopy, PreparedPagesFork,  # noqa: F401
+                     PreparedPagesFree, PreparedPagesGrow, qkn_pages_compact, qkn_pages_copy, qkn_pages_fork,
+                     qkn_pages_free, qkn_pages_grow)

@@ -23,7 +23,7 @@ SOURCES = [os.path.join(PKG_DIR, "csrc", name)
                         "qkn_kern_any.hip", "qkn_kern_once.hip", "qkn_kern_misc.hip", "qkn_proj.hip", "qkn_calib.hip",
                         "qkn_rope.hip", "qkn_attn.hip", "qkn_attn_few.hip", "qkn_attn_many.hip", "qkn_attn_few_sinks.hip",
                         "qkn_attn_many_sinks.hip", "qkn_attn_few4.hip", "qkn_attn_many4.hip",
-                        "qkn_cache4.hip", "qkn_adapters.hip")]
+                        "qkn_cache4.hip", "qkn_pages.hip", "qkn_adapters.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG_DIR, "libqkn.so")
 ARCH = "gfx950"
