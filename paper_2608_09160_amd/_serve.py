@@ -121,6 +121,10 @@ class KVCache:
     k_scale: Optional[torch.Tensor] = None
     v_scale: Optional[torch.Tensor] = None
 
+    @property
+    def head_dim(self) -> int:
+        return self.k.shape[3]
+
     def struct(self) -> QknCache:
         if self.k.dtype not in _CACHE_DTYPES or self.k.dtype != self.v.dtype:
             raise TypeError(f"cache: expected two pools in bf16 or float8_e4m3fn, got {self.k.dtype}, {self.v.dtype}")

@@ -8,21 +8,27 @@ serving loop runs it: every step on the library's kernels.
       -> attention over the cache                         qkn_attn
       -> this rank's term of the output projection        qkn_proj_partial
 
+The cache may be one in 4 bits (KVCache4), and a layer may have a window with first tokens that stay visible. Pages are
+handed out by the host (Pages) or by a book on the device (PageBook), which a captured decode loop grows by itself.
+
 A step's tensors are allocated once and its arguments checked once; the step then runs any number of times, by itself
 or captured in a HIP graph, on whatever x, positions, slots, lengths, page tables and adapter numbers hold then.
 
 ``python -m paper_2608_09160_amd.block`` serves a few sequences: prompts first, then single tokens from a replayed
-graph, and prints the time of a step.
+graph, and prints the time of a step; then one prompt in several branches over a 4-bit cache, with a window and first
+tokens, whose pages the device hands out.
 """
 from __future__ import annotations
 
 from dataclasses import dataclass
-from typing import Callable, Optional
+from typing import Callable, Optional, Union
 
 import torch
 
 from ._lib import PreparedProj, ProjSeg
-from ._serve import (AdapterSeg, KVCache, PreparedAdapters, PreparedAttn, PreparedRopeCache, RopeSeg, _on, qkn_rope_table)
+from ._pages import (PageBook, PreparedPagesGrow, qkn_pages_compact, qkn_pages_fork, qkn_pages_free, qkn_pages_grow)
+from ._serve import (AdapterSeg, KVCache, KVCache4, PreparedAdapters, PreparedAttn, PreparedRopeCache, RopeSeg, _on,
+                     qkn_rope_table)
 
 
 @dataclass
@@ -60,17 +66,18 @@ class Batch:
 class Step:
     """The block for batches of a given shape. exchange(stat_q, stat_k, rank): makes the other ranks' rows of the fp32
     [tp, T] statistics valid, this rank's row being so already (an all-gather in place); called between the kernels, on
-    the same stream. Not needed at tp = 1. `out` is this rank's term of the block's output, to be added over the ranks."""
+    the same stream. Not needed at tp = 1. `out` is this rank's term of the block's output, to be added over the ranks.
+    window: keys that a token sees (0: all), with the sequence's first `sinks` tokens besides."""
 
-    def __init__(self, w: Weights, cache: KVCache, table: torch.Tensor, batch: Batch, tp: int = 1, rank: int = 0,
-                 eps: float = 1e-6, window: int = 0, exchange: Optional[Callable] = None):
+    def __init__(self, w: Weights, cache: Union[KVCache, KVCache4], table: torch.Tensor, batch: Batch, tp: int = 1,
+                 rank: int = 0, eps: float = 1e-6, window: int = 0, exchange: Optional[Callable] = None, sinks: int = 0):
         if not 0 <= rank < tp:
             raise ValueError("rank must be one of tp")
         if tp > 1 and exchange is None:
             raise ValueError("exchange: needed with several ranks")
         if w.adapters is not None and batch.ids is None:
             raise ValueError("batch.ids: needed with adapters")
-        x, T, D = batch.x, batch.x.shape[0], cache.k.shape[3]
+        x, T, D = batch.x, batch.x.shape[0], cache.head_dim
         self.batch, self.tp, self.rank, self.exchange = batch, tp, rank, exchange
         # nothing is written here: the step may run on another stream than the current one
         self.stat_q, self.stat_k = (torch.empty(tp, T, dtype=torch.float32, device=x.device) for _ in range(2))
@@ -89,7 +96,7 @@ class Step:
             table, batch.pos, D, RopeSeg(self.q, w.gq, self.stat_q, tp * self.q.shape[1], self.q),
             RopeSeg(self.k, w.gk, self.stat_k, tp * self.k.shape[1]), self.v, cache, batch.slots, eps=eps)
         self.attn = PreparedAttn(self.q, cache, batch.block_table, batch.q_start, batch.kv_len, batch.max_q,
-                                 batch.max_kv, window=window)
+                                 batch.max_kv, window=window, sinks=sinks)
         o = ProjSeg(w.wo)
         self.output = PreparedProj(self.attn.out, [o])
         self.out = o.y
@@ -181,5 +188,71 @@ def main(prompts=(700, 64, 2048, 1), tokens: int = 16, hidden: int = 4096, heads
     return step.out
 
 
+def branches(prompt: int = 700, count: int = 4, tokens: int = 32, hidden: int = 4096, heads: int = 16, kv_heads: int = 4,
+             head_dim: int = 128, page_size: int = 16, window: int = 256, sinks: int = 4) -> tuple:
+    """Serves one prompt in `count` branches of `tokens` tokens each, half of which are dropped half way, over a 4-bit
+    cache. Returns the last step's output, the book and the cache."""
+    dev = torch.device("cuda")
+    g = torch.Generator().manual_seed(0)
+
+    def mat(*shape):
+        return (torch.randn(*shape, generator=g) * shape[-1] ** -0.5).to(torch.bfloat16).to(dev)
+
+    def ints(values):
+        return torch.tensor(list(values), dtype=torch.int32, device=dev)
+
+    n_q, n_kv = heads * head_dim, kv_heads * head_dim
+    w = Weights(mat(n_q, hidden), mat(n_kv, hidden), mat(n_kv, hidden), mat(hidden, n_q), torch.ones(n_q, device=dev),
+                torch.ones(n_kv, device=dev))
+    longest = prompt + tokens
+    # the prompt's pages once, and what each branch adds to them
+    pages = (prompt + page_size - 1) // page_size + count * (tokens // page_size + 2)
+    book = PageBook.empty(pages, count, longest, page_size, dev)
+    cache = KVCache4.empty(pages, kv_heads, page_size, head_dim, dev)
+    table = qkn_rope_table(longest, head_dim, device=dev)
+    mask = dict(window=window, sinks=sinks)
+
+    # the prompt, in row 0
+    slots, pos = torch.empty(prompt, dtype=torch.int64, device=dev), torch.empty(prompt, dtype=torch.int32, device=dev)
+    qkn_pages_grow(book, ints([prompt]), ints([0]), slots, pos)
+    x = torch.randn(prompt, hidden, generator=g).to(torch.bfloat16).to(dev)
+    out = Step(w, cache, table, Batch(x, pos, slots, ints([0, prompt]), book.kv_len[:1], book.table[:1], prompt, prompt),
+               **mask)()
+    qkn_pages_fork(book, ints([0] * (count - 1)), ints(range(1, count)), [cache])
+
+    # a token of each branch at a time: pages, slots and positions come from the device, in the same graph
+    more, start = ints([1] * count), ints(range(count + 1))
+    slots, pos = torch.empty(count, dtype=torch.int64, device=dev), torch.empty(count, dtype=torch.int32, device=dev)
+    grow = PreparedPagesGrow(book, more, slots=slots, pos=pos)
+    b = Batch((out[-1:] + 0.1 * torch.randn(count, hidden, generator=g).to(torch.bfloat16).to(dev)), pos, slots, start,
+              book.kv_len, book.table, 1, longest)
+    step = Step(w, cache, table, b, **mask)
+    grow()
+    step()  # the first token outside the capture
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        grow()
+        step()
+    begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    spent = 0.0
+    for i in range(1, tokens):
+        if i == tokens // 2:  # the later half of the branches ends: their tokens become padding, their pages free
+            kept = (count + 1) // 2
+            qkn_pages_free(book, ints(range(kept, count)))
+            more[kept:] = 0
+            start.clamp_(max=kept)
+            qkn_pages_compact(book, *(torch.empty(pages, dtype=torch.int32, device=dev) for _ in range(2)), [cache])
+        b.x.copy_(step.out)  # the model's other layers would stand here
+        begin.record()
+        graph.replay()
+        end.record()
+        torch.cuda.synchronize()
+        spent += begin.elapsed_time(end)
+    print(f"{count} branches of a prompt of {prompt}, 4-bit cache: {1e3 * spent / max(1, tokens - 1):.1f} us a step")
+    return step.out, book, cache
+
+
 if __name__ == "__main__":
     main()
+    branches()
