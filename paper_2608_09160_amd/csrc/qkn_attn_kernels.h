@@ -220,6 +220,7 @@ struct Tiles {
   int32_t sink_page, near_page, next0;
   const unsigned char* base_ke;  // FP4: the head's exponents of page 0
   const unsigned char* base_ve;
+  uint32_t k_off[C::KL], ke_off[C::KL], v_off[C::CODE_LOADS], ve_off[C::CODE_LOADS];  // FP4: this lane's part of each load
 
   __device__ __forceinline__ Tiles(const Params& pp, unsigned char* b, int l, int w) : buf(b), lane(l), wave(w), p(pp) {}
 
@@ -230,6 +231,7 @@ struct Tiles {
   // Takes 64 pages' places at once, a lane each: the address of a tile is then a few scalar instructions.
   __device__ __forceinline__ void hold(int32_t page) {
     if constexpr (C::FP4) {
+      asm volatile("" : "+v"(page));  // waited for here, not wherever a page is looked up
       k_lo = page;
       return;
     }
@@ -252,6 +254,14 @@ struct Tiles {
     if constexpr (C::FP4) {
       base_ke = p.ke.base + head * p.ke.head;
       base_ve = p.ve.base + head * p.ve.head;
+#pragma unroll
+      for (int x = 0; x < C::KL; ++x) {
+        if constexpr (C::SHARED) part4(p.k.token, p.ke.token, x * (64 / C::ROW_LANES) + lane / C::ROW_LANES, lane % C::ROW_LANES, k_off[x], ke_off[x]);
+        else part4(p.k.token, p.ke.token, lane & 15, 4 * x + (lane >> 4), k_off[x], ke_off[x]);
+      }
+#pragma unroll
+      for (int x = 0; x < C::CODE_LOADS; ++x)
+        part4(p.v.token, p.ve.token, x * (64 / C::ROW_LANES) + lane / C::ROW_LANES, lane % C::ROW_LANES, v_off[x], ve_off[x]);
     }
     if constexpr (C::SINKS) {
       sink_page = (sink_keys - 1) >> p.page_shift;
@@ -295,48 +305,51 @@ struct Tiles {
     u32x4 w[C::CODE_LOADS];
     uint32_t e[C::CODE_LOADS];
   };
-  // FP4: descriptors of the 16 rows' codes and exponents from key j on.
+  // FP4: the 16 rows from key j on, codes and exponents: of a page that is there all of it, else nothing. Rows of the page
+  // past the sequence's last are read with the others: no row sees them, and `put` takes out their NaN. Where nothing is
+  // `wanted` the loads still go out, and touch no memory: in a branch the compiler would wait for all of them behind it.
   template <bool V>
-  __device__ __forceinline__ void rows4_of(int32_t j, Rsrc& codes, Rsrc& exps) {
+  __device__ __forceinline__ void rows4_of(int32_t j, bool wanted, Rsrc& codes, Rsrc& exps) {
     const int32_t pi = j >> p.page_shift;
     hold_for(pi);
     const uint32_t page = static_cast<uint32_t>(__builtin_amdgcn_readlane(k_lo, pi - page0));
-    const int64_t row0 = j & ((1 << p.page_shift) - 1);
-    const int32_t left = kv_len - j, rows = left < 16 ? left : 16;
-    const bool none = left <= 0 || page >= p.num_pages;
+    const uint32_t row0 = j & ((1 << p.page_shift) - 1), bytes = wanted && j < kv_len && page < p.num_pages ? 0x7ffffffeu : 0u;
     const Pool& c = V ? p.v : p.k;
     const Exponents& e = V ? p.ve : p.ke;
-    const uint32_t c_bytes = __builtin_amdgcn_readfirstlane(none ? 0 : rows * c.token - (c.token - p.D / 2));
-    const uint32_t e_bytes = __builtin_amdgcn_readfirstlane(none ? 0 : rows * e.token - (e.token - p.D / 32));
-    codes = rsrc((V ? base_v : base_k) + (none ? 0 : page * c.page + row0 * c.token), c_bytes);
-    exps = rsrc((V ? base_ve : base_ke) + (none ? 0 : page * e.page + row0 * e.token), e_bytes);
+    codes = rsrc((V ? base_v : base_k) + (page * c.page + row0 * c.token), bytes);
+    exps = rsrc((V ? base_ve : base_ke) + (page * e.page + row0 * e.token), bytes);
   }
-  // Byte `at` of row r's codes, the exponent with it; past the head's end zeros.
-  template <bool V>
-  __device__ __forceinline__ void load4(Rsrc codes, Rsrc exps, int r, uint32_t at, u32x4& w, uint32_t& e) const {
+  // Where part `part` of row r of 16 is, its codes and their exponent; past the head's end beyond every buffer, which
+  // reads as zeros. Kept as it is: a choice that the loop makes anew would be a branch around each load.
+  __device__ __forceinline__ void part4(uint32_t token, uint32_t exp_token, int r, int part, uint32_t& off, uint32_t& exp_off) const {
+    const uint32_t at = part * C::LANE_CODES;
     const bool in = at < static_cast<uint32_t>(p.D / 2);
-    const uint32_t from = in ? r * (V ? p.v.token : p.k.token) + at : 0x7fffffffu;
+    off = in ? r * token + at : 0x7fffffffu;
+    exp_off = in ? r * exp_token + at / 16 : 0x7fffffffu;
+    asm volatile("" : "+v"(off), "+v"(exp_off));
+  }
+  __device__ __forceinline__ void load4(Rsrc codes, Rsrc exps, uint32_t off, uint32_t exp_off, u32x4& w, uint32_t& e) const {
     if constexpr (C::LANE_CODES == 16) {
-      w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, from, 0, 0));
+      w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, off, 0, 0));
     } else {
-      const u32x2 u = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, from, 0, 0));
+      const u32x2 u = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, off, 0, 0));
       w = u32x4{u[0], u[1], 0u, 0u};
     }
-    e = __builtin_amdgcn_raw_buffer_load_b8(exps, in ? r * (V ? p.ve.token : p.ke.token) + at / 16 : 0x7fffffffu, 0, 0);
+    e = __builtin_amdgcn_raw_buffer_load_b8(exps, exp_off, 0, 0);
   }
   // Requests the 16 rows from key j on; lane l has part l % ROW_LANES of row l / ROW_LANES (+ 64 / ROW_LANES a load).
   template <bool V>
-  __device__ __forceinline__ void fetch(int32_t j, Codes& x) {
+  __device__ __forceinline__ void fetch(int32_t j, bool wanted, Codes& x) {
     Rsrc codes, exps;
-    rows4_of<V>(j, codes, exps);
+    rows4_of<V>(j, wanted, codes, exps);
 #pragma unroll
     for (int i = 0; i < C::CODE_LOADS; ++i)
-      load4<V>(codes, exps, i * (64 / C::ROW_LANES) + lane / C::ROW_LANES, lane % C::ROW_LANES * C::LANE_CODES, x.w[i], x.e[i]);
+      load4(codes, exps, V ? v_off[i] : k_off[i], V ? ve_off[i] : ke_off[i], x.w[i], x.e[i]);
   }
-  // Writes such rows as bf16, row row0 of the K (V) tile in buffer `at` on. `finite`: 0 in the place of NaN; true if
-  // there was any.
+  // Writes such rows as bf16, row row0 of the K (V) tile in buffer `at` on; j is the first one's key. `finite`: 0 in the
+  // place of NaN; true if there was any in the sequence's rows.
   template <bool V>
-  __device__ __forceinline__ bool put(const Codes& x, int row0, int at, bool finite) {
+  __device__ __forceinline__ bool put(const Codes& x, int row0, int at, bool finite, int32_t j) {
     bool any = false;
 #pragma unroll
     for (int i = 0; i < C::CODE_LOADS; ++i) {
@@ -345,15 +358,15 @@ struct Tiles {
       const int chunk0 = lane % C::ROW_LANES * C::CODE_WORDS, swizzle = V ? C::swizzle_v(r) : C::swizzle_k(r);
       const bool nan = x.e[i] == 255;
       const bool some = __builtin_amdgcn_ballot_w64(nan);
-      any |= some;
+      if (some && finite) any |= __builtin_amdgcn_ballot_w64(nan && j + (r - row0) < kv_len) != 0;
 #pragma unroll
-      for (int e = 0; e < C::CODE_WORDS; ++e) {
-        u32x4 u = __builtin_bit_cast(u32x4, quant4::decode(x.w[i][e], x.e[i]));
-        if (some && nan) {
-          const uint32_t two = finite ? 0u : 0x7fc07fc0u;
-          u = u32x4{two, two, two, two};
-        }
-        *reinterpret_cast<u32x4*>(row + ((chunk0 + e) ^ swizzle) * 16) = u;
+      for (int e = 0; e < C::CODE_WORDS; ++e)
+        *reinterpret_cast<u32x4*>(row + ((chunk0 + e) ^ swizzle) * 16) = __builtin_bit_cast(u32x4, quant4::decode(x.w[i][e], x.e[i]));
+      if (some && nan) {
+        const uint32_t two = finite ? 0u : 0x7fc07fc0u;
+#pragma unroll
+        for (int e = 0; e < C::CODE_WORDS; ++e)
+          *reinterpret_cast<u32x4*>(row + ((chunk0 + e) ^ swizzle) * 16) = u32x4{two, two, two, two};
       }
     }
     return any;
@@ -391,14 +404,14 @@ struct Tiles {
     }
   }
   // FP4: the same; lane l has its codes of row l mod 16, bytes LANE_CODES (l / 16) .. of each 64 (heads of 64: 32).
-  __device__ __forceinline__ void request_k4(int32_t j0, u32x4 (&k)[C::KT / 16][C::KL], uint32_t (&e)[C::KT / 16][C::KL]) {
+  __device__ __forceinline__ void request_k4(int32_t j0, bool wanted, u32x4 (&k)[C::KT / 16][C::KL], uint32_t (&e)[C::KT / 16][C::KL]) {
 #pragma unroll
     for (int bl = 0; bl < C::KT / 16; ++bl) {
       Rsrc codes, exps;
-      rows4_of<false>(j0 + 16 * bl, codes, exps);
+      rows4_of<false>(j0 + 16 * bl, wanted, codes, exps);
 #pragma unroll
       for (int x = 0; x < C::KL; ++x)
-        load4<false>(codes, exps, lane & 15, C::LANE_CODES * (4 * x + (lane >> 4)), k[bl][x], e[bl][x]);
+        load4(codes, exps, k_off[x], ke_off[x], k[bl][x], e[bl][x]);
     }
   }
   // A weight of 0 times an infinite or NaN value is NaN, which a row that does not see the key must not get. In a
@@ -490,8 +503,7 @@ struct Rows {
   bf16x8 q[C::DT / 32][C::CB];
   f32x4 o[C::DT / 16][C::CB];   // O^T, this lane's elements 16 db + 4 (lane / 16) .. + 3
   float m[C::CB], l[C::CB];     // bound (of raw scores); sum over this lane's keys
-  int32_t lo[C::CB], hi[C::CB]; // the keys that the row sees,
-  int32_t first[C::CB];         // and (SINKS) those before this one
+  int32_t lo[C::CB], hi[C::CB]; // the keys that the row sees; SINKS: and the first ones below hi
 };
 
 template <class C>
@@ -542,7 +554,7 @@ __device__ __forceinline__ void scores(const Tiles<C>& t, const Rows<C>& w, cons
 // of the keys.
 template <class C>
 __device__ __forceinline__ void softmax(Rows<C>& w, Scores<C>& s, Weights<C>& pf, int lane, int32_t j0, float c,
-                                        bool masked) {
+                                        int32_t sinks_all, bool masked) {
   constexpr int KB = C::KT / 16, KC = C::KT / 32, ND = C::DT / 16;
   const int g = lane >> 4;
   if (masked) {
@@ -550,7 +562,7 @@ __device__ __forceinline__ void softmax(Rows<C>& w, Scores<C>& s, Weights<C>& pf
     for (int cb = 0; cb < C::CB; ++cb) {
       const uint32_t seen = static_cast<uint32_t>(w.hi[cb] - w.lo[cb]);
       const int32_t first = j0 + 4 * g - w.lo[cb];
-      const int32_t sinks = C::SINKS ? w.first[cb] - (j0 + 4 * g) : 0;
+      const int32_t sinks = C::SINKS ? (sinks_all < w.hi[cb] ? sinks_all : w.hi[cb]) - (j0 + 4 * g) : 0;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -655,7 +667,7 @@ __device__ __forceinline__ void add_infinities(const Tiles<C>& t, Rows<C>& w, in
         if (__builtin_isfinite(v)) continue;
 #pragma unroll
         for (int cb = 0; cb < C::CB; ++cb)
-          if ((j >= w.lo[cb] && j < w.hi[cb]) || (C::SINKS && j < w.first[cb])) w.o[db][cb][r] += v;
+          if ((j >= w.lo[cb] && j < w.hi[cb]) || (C::SINKS && j < t.p.sinks && j < w.hi[cb])) w.o[db][cb][r] += v;
       }
     }
   }
@@ -878,7 +890,6 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
     const Range x = range(r, r);
     w.lo[cb] = x.lo;
     w.hi[cb] = x.hi;
-    if constexpr (C::SINKS) w.first[cb] = sinks_below(x.hi);
     w.m[cb] = neg_inf();
     w.l[cb] = 0.0f;
     const uint16_t* src = p.q + at_t[cb] * p.ldq + static_cast<int64_t>(at_h[cb]) * p.D;
@@ -926,28 +937,26 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
       typename Tiles<C>::Codes ck, cv;
       const auto fetch = [&](int32_t i) {
         const int32_t j = key_of(i) + t.first_row(0);
-        t.template fetch<false>(j, ck);
-        t.template fetch<true>(j, cv);
+        t.template fetch<false>(j, i < count, ck);
+        t.template fetch<true>(j, i < count, cv);
       };
       const auto put = [&](int32_t i) {
-        t.template put<false>(ck, t.first_row(0), i & 1, false);
-        const bool some = in_part(key_of(i));
-        if (t.template put<true>(cv, t.first_row(0), i & 1, some) && some) any_infinite = 1;
+        const int32_t j = key_of(i) + t.first_row(0);
+        t.template put<false>(ck, t.first_row(0), i & 1, false, j);
+        if (t.template put<true>(cv, t.first_row(0), i & 1, in_part(key_of(i)), j)) any_infinite = 1;
       };
       fetch(0);
       put(0);
-      if (count > 1) fetch(1);
+      fetch(1);
       for (int32_t i = 0; i < count; ++i) {
         const int32_t j0 = key_of(i);
         __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): this wavefront's rows of tile i are written,
         group_barrier();                     // every wavefront's are, and all have read tile i - 1
-        if (i + 1 < count) {
-          put(i + 1);
-          if (i + 2 < count) fetch(i + 2);
-        }
+        if (i + 1 < count) put(i + 1);
+        fetch(i + 2);
         if (sees(j0)) {
           scores(t, w, kr, ke, i & 1, sc);
-          softmax(w, sc, pf, lane, j0, c, masked(j0));
+          softmax(w, sc, pf, lane, j0, c, p.sinks, masked(j0));
           product(t, w, pf, i & 1);
         }
       }
@@ -965,30 +974,28 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
         }
         if (sees(j0)) {
           scores(t, w, kr, ke, i & 1, sc);
-          softmax(w, sc, pf, lane, j0, c, masked(j0));
+          softmax(w, sc, pf, lane, j0, c, p.sinks, masked(j0));
           product(t, w, pf, i & 1);
         }
       }
     } else if constexpr (C::FP4) {
       typename Tiles<C>::Codes cv[C::KT / 16];
-      const auto fetch = [&](int32_t j) {
+      const auto fetch = [&](int32_t i) {
 #pragma unroll
-        for (int bl = 0; bl < C::KT / 16; ++bl) t.template fetch<true>(j + 16 * bl, cv[bl]);
+        for (int bl = 0; bl < C::KT / 16; ++bl) t.template fetch<true>(key_of(i) + 16 * bl, i < count, cv[bl]);
       };
-      if (wave < count) {
-        fetch(key_of(wave));
-        t.request_k4(key_of(wave), kr, ke);
-      }
+      fetch(wave);
+      t.request_k4(key_of(wave), wave < count, kr, ke);
       for (int32_t i = wave; i < count; i += C::WAVES) {
-        const int32_t j0 = key_of(i), j1 = key_of(i + C::WAVES);
-        const bool more = i + C::WAVES < count, some = in_part(j0);
+        const int32_t j0 = key_of(i), next = i + C::WAVES;
+        const bool some = in_part(j0);
 #pragma unroll
         for (int bl = 0; bl < C::KT / 16; ++bl)
-          if (t.template put<true>(cv[bl], 16 * bl, 0, some) && some) any_infinite = 1;
-        if (more) fetch(j1);
+          if (t.template put<true>(cv[bl], 16 * bl, 0, some, j0 + 16 * bl)) any_infinite = 1;
+        fetch(next);
         scores(t, w, kr, ke, 0, sc);
-        if (more) t.request_k4(j1, kr, ke);  // the registers are free
-        softmax(w, sc, pf, lane, j0, c, masked(j0));
+        t.request_k4(key_of(next), next < count, kr, ke);  // the registers are free
+        softmax(w, sc, pf, lane, j0, c, p.sinks, masked(j0));
         product(t, w, pf, 0);
         asm volatile("" ::: "memory");  // the next rows are written where this tile was read
         __builtin_amdgcn_sched_barrier(0);
@@ -1011,7 +1018,7 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
         if (in_part(j0) && t.make_finite(at)) any_infinite = 1;
         scores(t, w, kr, ke, at, sc);
         if (more) t.request_k(j1, kr);  // the registers are free
-        softmax(w, sc, pf, lane, j0, c, masked(j0));
+        softmax(w, sc, pf, lane, j0, c, p.sinks, masked(j0));
         product(t, w, pf, at);
         asm volatile("" ::: "memory");  // the next request writes where this tile was read
         __builtin_amdgcn_sched_barrier(0);
