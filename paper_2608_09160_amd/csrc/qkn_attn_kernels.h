@@ -242,10 +242,12 @@ struct Tiles {
     v_lo = static_cast<int32_t>(v);
     v_hi = static_cast<int32_t>(v >> 32);
   }
-  // The 64 pages behind those from page `p0` on that the rows need.
+  // The 64 pages that the rows need behind those from page `p0` on. FP4: pages are held for a tile (hold_for), whose
+  // pages, up to KT / 16, must be held together.
+  static constexpr int NEXT = C::FP4 ? 64 - C::KT / 16 : 64;
   __device__ __forceinline__ int32_t after(int32_t p0) const {
-    if constexpr (C::SINKS) return p0 + 64 > sink_page && p0 + 64 < near_page ? near_page : p0 + 64;
-    else return p0 + 64;
+    if constexpr (C::SINKS) return p0 + NEXT > sink_page && p0 + NEXT < near_page ? near_page : p0 + NEXT;
+    else return p0 + NEXT;
   }
   // sink_keys: the tiles of the first keys end there (0: none); near_key: the windows' begin there.
   __device__ __forceinline__ void open(int b, int head, int32_t m, int32_t first_key, int32_t sink_keys, int32_t near_key) {
@@ -271,15 +273,16 @@ struct Tiles {
     table = p.table + b * p.ld_table;
     last_page = (m - 1) >> p.page_shift;
     page0 = first_key >> p.page_shift;
-    const int32_t first = entry(page0 + lane);
+    k_lo = entry(page0 + lane);
     next0 = after(page0);
     next = entry(next0 + lane);
-    hold(first);
   }
+  // Waits for the first pages' numbers, which `open` asks for.
+  __device__ __forceinline__ void begin() { hold(k_lo); }
   __device__ __forceinline__ void hold_for(int32_t page) {
     while (page - page0 >= 64) {  // pages are taken in ascending order
       hold(next);
-      page0 = next0;
+      page0 = C::SINKS ? next0 : page0 + NEXT;
       next0 = after(page0);
       next = entry(next0 + lane);
     }
@@ -311,7 +314,6 @@ struct Tiles {
   template <bool V>
   __device__ __forceinline__ void rows4_of(int32_t j, bool wanted, Rsrc& codes, Rsrc& exps) {
     const int32_t pi = j >> p.page_shift;
-    hold_for(pi);
     const uint32_t page = static_cast<uint32_t>(__builtin_amdgcn_readlane(k_lo, pi - page0));
     const uint32_t row0 = j & ((1 << p.page_shift) - 1), bytes = wanted && j < kv_len && page < p.num_pages ? 0x7ffffffeu : 0u;
     const Pool& c = V ? p.v : p.k;
@@ -337,6 +339,8 @@ struct Tiles {
     }
     e = __builtin_amdgcn_raw_buffer_load_b8(exps, exp_off, 0, 0);
   }
+  // Before the requests of the tile at key j, whose pages come in ascending order.
+  __device__ __forceinline__ void hold_tile(int32_t j) { hold_for((j + C::KT - 1) >> p.page_shift); }
   // Requests the 16 rows from key j on; lane l has part l % ROW_LANES of row l / ROW_LANES (+ 64 / ROW_LANES a load).
   template <bool V>
   __device__ __forceinline__ void fetch(int32_t j, bool wanted, Codes& x) {
@@ -740,7 +744,20 @@ __device__ __forceinline__ bool schedule(const Params& p, int lane, int32_t idx,
     }
     return Need{(mine.n * G + C::BM - 1) / C::BM, steps};
   };
-  const auto parts = [](const Need& x, int32_t per) { return x.steps > per ? (x.steps + per - 1) / per : 1; };
+  const auto parts = [](const Need& x, int32_t per) {
+    // (steps + per - 1) / per, which takes 30 instructions; up to 2^22 the product with the reciprocal is off by less than
+    // one
+    const uint32_t n = static_cast<uint32_t>(x.steps) + static_cast<uint32_t>(per) - 1, d = static_cast<uint32_t>(per);
+    uint32_t q;
+    if (__builtin_amdgcn_ballot_w64(n >= 1u << 22)) {
+      q = n / d;
+    } else {
+      q = static_cast<uint32_t>(static_cast<float>(n) * __builtin_amdgcn_rcpf(static_cast<float>(d)));
+      const int32_t rest = static_cast<int32_t>(n - q * d);
+      q += rest >= static_cast<int32_t>(d) ? 1 : rest < 0 ? -1 : 0;
+    }
+    return x.steps > per ? static_cast<int32_t>(q) : 1;
+  };
   Need x = need(0);
   it.first = __builtin_amdgcn_readlane(mine.q0, 0);
   it.end = 0;
@@ -755,11 +772,17 @@ __device__ __forceinline__ bool schedule(const Params& p, int lane, int32_t idx,
     per = per < p.min_part ? p.min_part : per;
     if (p.batch > 64) x = need(0);
   }
+  int32_t own_parts = 0, own_upto = 0;  // of the first 64 sequences
   while (true) {
     count = 0;
     for (int base = 0; base < p.batch; base += 64) {
       if (base) x = need(base);
-      count += last_lane(lane_sums(x.tiles * parts(x, per)));
+      const int32_t n = parts(x, per), upto = lane_sums(x.tiles * n);
+      count += last_lane(upto);
+      if (base == 0) {
+        own_parts = n;
+        own_upto = upto;
+      }
       const int32_t last = p.batch - 1 - base;
       it.end = __builtin_amdgcn_readlane(mine.q0 + mine.n, last < 63 ? last : 63);
     }
@@ -774,13 +797,13 @@ __device__ __forceinline__ bool schedule(const Params& p, int lane, int32_t idx,
   if (left < 0) return false;
   for (int base = 0; base < p.batch; base += 64) {
     if (base) x = need(base);
-    const int32_t own = x.tiles * parts(x, per), upto = lane_sums(own);
+    const int32_t n = base ? parts(x, per) : own_parts, own = x.tiles * n, upto = base ? lane_sums(own) : own_upto;
     const uint64_t after = __builtin_amdgcn_ballot_w64(upto > left);
     if (after) {
       const int at = __builtin_ctzll(after);
       const auto of = [&](int32_t v) { return __builtin_amdgcn_readlane(v, at); };
       it.b = base + at;
-      it.parts = of(parts(x, per));
+      it.parts = of(n);
       it.per = per;
       const int32_t in = left - (of(upto) - of(own));
       it.tile = in / it.parts;
@@ -871,6 +894,9 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
   };
   const auto sinks_below = [&](int32_t hi) { return p.sinks < hi ? p.sinks : hi; };
 
+  Tiles<C> t(p, lds + (C::SHARED ? 0 : wave * C::BUFFERS * C::BUF), lane, wave);
+  if (!C::SHARED && count > 0) t.open(b, head, m, key_of(0), apart, step0 * C::STEP);
+
   // rows of this wavefront
   const int32_t w0 = row0 + (C::SHARED ? wave * 16 * C::CB : 0);
   const int32_t w1 = w0 + 16 * C::CB < R ? w0 + 16 * C::CB : R;
@@ -930,13 +956,14 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
   if (threadIdx.x == 0) any_infinite = 0;
   __syncthreads();
   if (count > 0) {
-    Tiles<C> t(p, lds + (C::SHARED ? 0 : wave * C::BUFFERS * C::BUF), lane, wave);
-    t.open(b, head, m, key_of(0), apart, step0 * C::STEP);
+    if (C::SHARED) t.open(b, head, m, key_of(0), apart, step0 * C::STEP);
+    t.begin();
     if constexpr (C::SHARED && C::FP4) {
       // codes to registers a tile ahead, from there as bf16 to LDS
       typename Tiles<C>::Codes ck, cv;
       const auto fetch = [&](int32_t i) {
         const int32_t j = key_of(i) + t.first_row(0);
+        t.hold_tile(key_of(i));
         t.template fetch<false>(j, i < count, ck);
         t.template fetch<true>(j, i < count, cv);
       };
@@ -981,6 +1008,7 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
     } else if constexpr (C::FP4) {
       typename Tiles<C>::Codes cv[C::KT / 16];
       const auto fetch = [&](int32_t i) {
+        t.hold_tile(key_of(i));
 #pragma unroll
         for (int bl = 0; bl < C::KT / 16; ++bl) t.template fetch<true>(key_of(i) + 16 * bl, i < count, cv[bl]);
       };
