@@ -280,7 +280,7 @@ struct Tiles {
   // Waits for the first pages' numbers, which `open` asks for.
   __device__ __forceinline__ void begin() { hold(k_lo); }
   __device__ __forceinline__ void hold_for(int32_t page) {
-    while (page - page0 >= 64) {  // pages are taken in ascending order
+    while (__builtin_expect(page - page0 >= 64, 0)) {  // pages are taken in ascending order
       hold(next);
       page0 = C::SINKS ? next0 : page0 + NEXT;
       next0 = after(page0);
@@ -362,11 +362,11 @@ struct Tiles {
       const int chunk0 = lane % C::ROW_LANES * C::CODE_WORDS, swizzle = V ? C::swizzle_v(r) : C::swizzle_k(r);
       const bool nan = x.e[i] == 255;
       const bool some = __builtin_amdgcn_ballot_w64(nan);
-      if (some && finite) any |= __builtin_amdgcn_ballot_w64(nan && j + (r - row0) < kv_len) != 0;
+      if (__builtin_expect(some && finite, 0)) any |= __builtin_amdgcn_ballot_w64(nan && j + (r - row0) < kv_len) != 0;
 #pragma unroll
       for (int e = 0; e < C::CODE_WORDS; ++e)
         *reinterpret_cast<u32x4*>(row + ((chunk0 + e) ^ swizzle) * 16) = __builtin_bit_cast(u32x4, quant4::decode(x.w[i][e], x.e[i]));
-      if (some && nan) {
+      if (__builtin_expect(some, 0)) if (nan) {
         const uint32_t two = finite ? 0u : 0x7fc07fc0u;
 #pragma unroll
         for (int e = 0; e < C::CODE_WORDS; ++e)
@@ -561,7 +561,7 @@ __device__ __forceinline__ void softmax(Rows<C>& w, Scores<C>& s, Weights<C>& pf
                                         int32_t sinks_all, bool masked) {
   constexpr int KB = C::KT / 16, KC = C::KT / 32, ND = C::DT / 16;
   const int g = lane >> 4;
-  if (masked) {
+  if (__builtin_expect(masked, 0)) {
 #pragma unroll
     for (int cb = 0; cb < C::CB; ++cb) {
       const uint32_t seen = static_cast<uint32_t>(w.hi[cb] - w.lo[cb]);
@@ -589,7 +589,7 @@ __device__ __forceinline__ void softmax(Rows<C>& w, Scores<C>& s, Weights<C>& pf
     top[cb] = x;
     raise |= (x - w.m[cb]) * c > kSlack;  // m = -infinity: any score (+infinity), or none (NaN: false)
   }
-  if (__builtin_amdgcn_ballot_w64(raise)) {
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(raise) != 0, 0)) {
 #pragma unroll
     for (int cb = 0; cb < C::CB; ++cb) {
       float x = fmaxf(top[cb], w.m[cb]);
@@ -970,7 +970,7 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
       const auto put = [&](int32_t i) {
         const int32_t j = key_of(i) + t.first_row(0);
         t.template put<false>(ck, t.first_row(0), i & 1, false, j);
-        if (t.template put<true>(cv, t.first_row(0), i & 1, in_part(key_of(i)), j)) any_infinite = 1;
+        if (__builtin_expect(t.template put<true>(cv, t.first_row(0), i & 1, in_part(key_of(i)), j), 0)) any_infinite = 1;
       };
       fetch(0);
       put(0);
@@ -993,7 +993,7 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
       for (int32_t i = 0; i < count; ++i) {
         const int32_t j0 = key_of(i);
         wait_loads<0>();   // this wavefront's rows of tile i are there,
-        if (in_part(j0) && t.make_finite(i & 1)) any_infinite = 1;
+        if (__builtin_expect(in_part(j0), 0) && t.make_finite(i & 1)) any_infinite = 1;
         group_barrier();   // every wavefront's are, and all have read tile i - 1
         if (i + 1 < count) {
           t.template request<false>(key_of(i + 1), (i + 1) & 1);
@@ -1019,7 +1019,7 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
         const bool some = in_part(j0);
 #pragma unroll
         for (int bl = 0; bl < C::KT / 16; ++bl)
-          if (t.template put<true>(cv[bl], 16 * bl, 0, some, j0 + 16 * bl)) any_infinite = 1;
+          if (__builtin_expect(t.template put<true>(cv[bl], 16 * bl, 0, some, j0 + 16 * bl), 0)) any_infinite = 1;
         fetch(next);
         scores(t, w, kr, ke, 0, sc);
         t.request_k4(key_of(next), next < count, kr, ke);  // the registers are free
@@ -1043,7 +1043,7 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
         } else {
           wait_loads<0>();
         }
-        if (in_part(j0) && t.make_finite(at)) any_infinite = 1;
+        if (__builtin_expect(in_part(j0), 0) && t.make_finite(at)) any_infinite = 1;
         scores(t, w, kr, ke, at, sc);
         if (more) t.request_k(j1, kr);  // the registers are free
         softmax(w, sc, pf, lane, j0, c, p.sinks, masked(j0));
