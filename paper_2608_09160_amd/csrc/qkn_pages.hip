@@ -19,27 +19,47 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------ sums over a workgroup
 
-__device__ __forceinline__ int64_t wave_sums(int64_t x) {  // inclusive
-  const int lane = static_cast<int>(threadIdx.x) & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t y = __shfl_up(static_cast<long long>(x), d);
-    x += lane >= d ? y : 0;
-  }
-  return x;
+// x plus what lanes further back have (DPP: through no memory).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t add_from(uint32_t x) {
+  return x + static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), CTRL, ROWS, 0xf, false));
 }
+__device__ __forceinline__ uint32_t wave_sums(uint32_t x) {  // inclusive
+  x = add_from<0x111, 0xf>(x);  // 1, 2, 4, 8 lanes back in the row of 16
+  x = add_from<0x112, 0xf>(x);
+  x = add_from<0x114, 0xf>(x);
+  x = add_from<0x118, 0xf>(x);
+  x = add_from<0x142, 0xa>(x);     // the end of row 0 (2) into row 1 (3)
+  return add_from<0x143, 0xc>(x);  // the end of row 1 into rows 2 and 3
+}
+
+// Two 32-bit numbers that are summed side by side.
+struct Pair {
+  uint32_t a, b;
+};
+__device__ __forceinline__ Pair operator+(Pair x, Pair y) { return Pair{x.a + y.a, x.b + y.b}; }
+__device__ __forceinline__ Pair operator-(Pair x, Pair y) { return Pair{x.a - y.a, x.b - y.b}; }
+// Sums of up to 1024 numbers below 2^31, whose 20 lower bits and the rest are summed apart.
+__device__ __forceinline__ Pair apart(int64_t x) {
+  return Pair{static_cast<uint32_t>(x) & 0xfffffu, static_cast<uint32_t>(x >> 20)};
+}
+__device__ __forceinline__ int64_t together(Pair x) { return (static_cast<int64_t>(x.b) << 20) + x.a; }
+
 // Inclusive sums over the threads, and the sum of all. `room`: one value a wavefront; free again behind the next barrier.
 template <int WAVES>
-__device__ __forceinline__ int64_t group_sums(int64_t x, int64_t (&room)[WAVES], int64_t& all) {
-  const int wave = static_cast<int>(threadIdx.x) >> 6;
-  const int64_t s = wave_sums(x);
-  if ((threadIdx.x & 63) == 63) room[wave] = s;
+__device__ __forceinline__ Pair group_sums(Pair x, Pair (&room)[WAVES], Pair& all) {
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = static_cast<int>(threadIdx.x) & 63;
+  const Pair s = {wave_sums(x.a), wave_sums(x.b)};
+  if (lane == 63) room[wave] = s;
   __syncthreads();
-  const int lane = static_cast<int>(threadIdx.x) & 63;
-  const int64_t waves = wave_sums(lane < WAVES ? room[lane] : 0);  // those up to each
-  const int64_t before = __shfl(static_cast<long long>(waves), wave ? wave - 1 : 0);
-  all = __shfl(static_cast<long long>(waves), WAVES - 1);
-  return s + (wave ? before : 0);
+  const Pair w = lane < WAVES ? room[lane] : Pair{0, 0};
+  const Pair upto = {wave_sums(w.a), wave_sums(w.b)};  // those up to each wavefront
+  const auto at = [&](int l) {
+    return Pair{static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(upto.a), l)),
+                static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(upto.b), l))};
+  };
+  all = at(WAVES - 1);
+  return wave ? s + at(wave - 1) : s;
 }
 
 // ------------------------------------------------------------------ taking pages
@@ -66,6 +86,16 @@ struct TakeParams {
   int32_t *src, *dst, *done;
 };
 
+// refs[at .. at + 3]; past the end `past`. at is a multiple of 4, refs of 4 bytes' alignment at least.
+__device__ __forceinline__ i32x4 refs_at(const int32_t* refs, int64_t at, int64_t num_pages, int32_t past) {
+  typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+  if (at + 4 <= num_pages) return *reinterpret_cast<const i32x4_any*>(refs + at);
+  i32x4 r;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) r[e] = at + e < num_pages ? refs[at + e] : past;
+  return r;
+}
+
 __device__ __forceinline__ int64_t pages_for(int64_t tokens, int shift) { return (tokens + (int64_t{1} << shift) - 1) >> shift; }
 
 // The first i with upto[i] > r: upto ascending, r below the last.
@@ -79,15 +109,49 @@ __device__ __forceinline__ int holder(const int32_t* upto, int n, int32_t r) {
   return lo;
 }
 
+// Slots and positions of the tokens t0, t0 + THREADS, ..: four, or (T up to kMany) all. A token's table entry is a trip to
+// memory, so four go out together.
+template <int THREADS>
+__device__ __forceinline__ void list_tokens(const TakeParams& p, const int32_t* rows, const int32_t* length, const int32_t* first,
+                                            const int32_t* tokens, int64_t all, int64_t t0) {
+  const int shift = p.b.page_shift;
+  int32_t pos[4], page[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    const int64_t t = t0 + x * THREADS;
+    pos[x] = 0;
+    page[x] = -1;
+    if (t >= p.T || t >= all) continue;
+    const int at = holder(tokens, p.n, static_cast<int32_t>(t));
+    if (first[at] < 0) continue;  // refused
+    pos[x] = length[at] + static_cast<int32_t>(t - (at ? tokens[at - 1] : 0));
+    page[x] = p.b.table[rows[at] * p.b.ld_table + (pos[x] >> shift)];
+  }
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    const int64_t t = t0 + x * THREADS;
+    if (t >= p.T) break;
+    if (p.slots) p.slots[t] = page[x] < 0 ? -1 : (static_cast<int64_t>(page[x]) << shift) + (pos[x] & ((1 << shift) - 1));
+    if (p.pos) p.pos[t] = pos[x];
+  }
+}
+
 // One workgroup, thread i for entry i of the list. Sums that pass 2^31 are cut: no pool has as many pages, no list that
 // is written as many tokens.
 template <bool FORK>
 __global__ __launch_bounds__(kMost) void qkn_pages_take(const TakeParams p) {
-  __shared__ int64_t room[2][kTakeWaves];
+  __shared__ Pair room[2][kTakeWaves];
   __shared__ __align__(16) int32_t rows[kMost];
   __shared__ int32_t upto[kMost], first[kMost], tokens[kMost], length[kMost];
   const int i = static_cast<int>(threadIdx.x), shift = p.b.page_shift;
   const int64_t most = p.b.ld_table << shift;
+  // the first pages' counts are asked for before they are needed
+  i32x4 r[4];
+  const auto ask = [&](int64_t base) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) r[k] = refs_at(p.b.refs, base + (k * kMost + i) * 4, p.b.num_pages, 1);
+  };
+  ask(0);
   const auto cut = [](int64_t x) { return static_cast<int32_t>(x < 0x7fffffff ? x : 0x7fffffff); };
 
   const int32_t row = i >= p.n ? -1 : p.which ? p.which[i] : i;
@@ -109,9 +173,10 @@ __global__ __launch_bounds__(kMost) void qkn_pages_take(const TakeParams p) {
   }
   const int64_t have = FORK ? len >> shift : pages_for(len, shift);
   const int64_t need = fine ? pages_for(len + more, shift) - have : 0;
-  int64_t total, all_tokens;
-  const int64_t ends = group_sums<kTakeWaves>(need, room[0], total);
-  const int64_t token_end = FORK ? 0 : group_sums<kTakeWaves>(more, room[1], all_tokens);
+  Pair all_needs, all_more = {0, 0};
+  const int64_t ends = together(group_sums<kTakeWaves>(apart(need), room[0], all_needs)), total = together(all_needs);
+  const int64_t token_end = FORK ? 0 : together(group_sums<kTakeWaves>(apart(more), room[1], all_more));
+  const int64_t all_tokens = together(all_more);
   upto[i] = cut(ends);
   first[i] = static_cast<int32_t>(have);
   length[i] = static_cast<int32_t>(len);
@@ -121,27 +186,18 @@ __global__ __launch_bounds__(kMost) void qkn_pages_take(const TakeParams p) {
   // free pages, lowest first, to the needs in order
   int64_t found = 0;
   for (int64_t base = 0; base < p.b.num_pages && found < total; base += 16 * kMost) {
-    i32x4 r[4];
+    if (base) ask(base);
+    uint32_t c[4];  // free pages of this thread, of each k
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int64_t at = base + (k * kMost + i) * 4;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) r[k][e] = at + e < p.b.num_pages ? p.b.refs[at + e] : 1;
-    }
-    int64_t counts = 0;  // of each k in 16 bits
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      int c = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) c += r[k][e] == 0;
-      counts |= static_cast<int64_t>(c) << (16 * k);
-    }
-    int64_t all;
-    const int64_t before = group_sums<kTakeWaves>(counts, room[0], all) - counts;
+    for (int k = 0; k < 4; ++k) c[k] = (r[k][0] == 0) + (r[k][1] == 0) + (r[k][2] == 0) + (r[k][3] == 0);
+    const Pair counts = {c[0] | c[1] << 16, c[2] | c[3] << 16};  // up to 4096 each in 16 bits
+    Pair all;
+    const Pair before = group_sums<kTakeWaves>(counts, room[0], all) - counts;
     int64_t start = found;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      int64_t rank = start + ((before >> (16 * k)) & 0xffff);
+      const int half = 16 * (k % 2);
+      int64_t rank = start + (((k < 2 ? before.a : before.b) >> half) & 0xffff);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (r[k][e] != 0) continue;
@@ -155,7 +211,7 @@ __global__ __launch_bounds__(kMost) void qkn_pages_take(const TakeParams p) {
         }
         ++rank;
       }
-      start += (all >> (16 * k)) & 0xffff;
+      start += ((k < 2 ? all.a : all.b) >> half) & 0xffff;
     }
     found = start;
     __syncthreads();  // room
@@ -175,24 +231,41 @@ __global__ __launch_bounds__(kMost) void qkn_pages_take(const TakeParams p) {
     }
   }
   if constexpr (!FORK) {
-    if (!p.slots && !p.pos) return;
+    if ((!p.slots && !p.pos) || p.T > 4 * kMost) return;  // qkn_pages_slots
     if (!served) first[i] = -1;
     __syncthreads();
-    for (int64_t t = i; t < p.T; t += kMost) {
-      int64_t slot = -1;
-      int32_t at_pos = 0;
-      if (t < all_tokens) {
-        const int at = holder(tokens, p.n, static_cast<int32_t>(t));
-        if (first[at] >= 0) {
-          at_pos = length[at] + static_cast<int32_t>(t - (at ? tokens[at - 1] : 0));
-          slot = (static_cast<int64_t>(p.b.table[rows[at] * p.b.ld_table + (at_pos >> shift)]) << shift) +
-                 (at_pos & ((1 << shift) - 1));
-        }
-      }
-      if (p.slots) p.slots[t] = slot;
-      if (p.pos) p.pos[t] = at_pos;
-    }
+    list_tokens<kMost>(p, rows, length, first, tokens, all_tokens, i);
   }
+}
+
+// The slots of many new tokens, kMany a workgroup: what the workgroup above knows of the rows is found again.
+constexpr int kManyThreads = 256, kMany = 4 * kManyThreads;
+__global__ __launch_bounds__(kManyThreads) void qkn_pages_slots(const TakeParams p) {
+  __shared__ Pair room[kManyThreads / 64];
+  __shared__ int32_t rows[kMost], first[kMost], tokens[kMost], length[kMost];
+  const int i0 = 4 * static_cast<int>(threadIdx.x);
+  int64_t count[4], sum = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int i = i0 + e;
+    const int32_t c = i < p.n ? p.count[i] : 0, done = i < p.n ? p.done[i] : -1;
+    count[e] = c < 0 ? 0 : c;
+    sum += count[e];
+    rows[i] = i >= p.n ? -1 : p.which ? p.which[i] : i;
+    first[i] = done < 0 ? -1 : 0;
+    length[i] = static_cast<int32_t>(done - count[e]);
+  }
+  // up to four numbers below 2^31 a thread: the lower parts' sums stay below 2^32
+  Pair all_more;
+  int64_t end = together(group_sums<kManyThreads / 64>(apart(sum), room, all_more)) - sum;
+  const int64_t all = together(all_more);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    end += count[e];
+    tokens[i0 + e] = static_cast<int32_t>(end < 0x7fffffff ? end : 0x7fffffff);
+  }
+  __syncthreads();
+  list_tokens<kManyThreads>(p, rows, length, first, tokens, all, static_cast<int64_t>(blockIdx.x) * kMany + threadIdx.x);
 }
 
 // The whole pages of forked rows: 1024 entries of a row a workgroup.
@@ -236,46 +309,60 @@ struct MoveParams {
   Book b, out;
   int32_t *src, *dst;
   int32_t n;
-  int32_t* counts;   // pages in use of each kScan pages
+  int32_t* counts;   // pages in use of each kScan pages (more than kFewBlocks of them); the last one: moves
   int32_t* moved;    // [num_pages]: its move, -1: stays, -2: a move's end
   int32_t blocks;
 };
 
-__device__ __forceinline__ void used_of(const MoveParams& p, bool (&used)[4], int64_t& at) {
-  at = static_cast<int64_t>(blockIdx.x) * kScan + 4 * threadIdx.x;
+__device__ __forceinline__ int used_of(const MoveParams& p, int block, bool (&used)[4], int64_t& at) {
+  at = static_cast<int64_t>(block) * kScan + 4 * threadIdx.x;
+  const i32x4 r = refs_at(p.b.refs, at, p.b.num_pages, 0);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) used[e] = at + e < p.b.num_pages && p.b.refs[at + e] != 0;
+  for (int e = 0; e < 4; ++e) used[e] = r[e] != 0;
+  return used[0] + used[1] + used[2] + used[3];
 }
+// Up to so many blocks of pages, each workgroup counts all of them itself: a launch less.
+constexpr int kFewBlocks = 16;
 
 __global__ __launch_bounds__(kScanThreads) void qkn_pages_count(const MoveParams p) {
-  __shared__ int64_t room[kScanWaves];
+  __shared__ Pair room[kScanWaves];
   bool used[4];
-  int64_t at, all;
-  used_of(p, used, at);
-  group_sums<kScanWaves>(used[0] + used[1] + used[2] + used[3], room, all);
-  if (threadIdx.x == 0) p.counts[blockIdx.x] = static_cast<int32_t>(all);
-  for (int64_t k = static_cast<int64_t>(blockIdx.x) * kScanThreads + threadIdx.x; k < p.n;
-       k += static_cast<int64_t>(p.blocks) * kScanThreads)
-    p.src[k] = p.dst[k] = -1;
+  int64_t at;
+  Pair all;
+  const int c = used_of(p, static_cast<int>(blockIdx.x), used, at);
+  group_sums<kScanWaves>(Pair{static_cast<uint32_t>(c), 0}, room, all);
+  if (threadIdx.x == 0) p.counts[blockIdx.x] = static_cast<int32_t>(all.a);
 }
 
 __global__ __launch_bounds__(kScanThreads) void qkn_pages_moves(const MoveParams p) {
-  __shared__ int64_t room[3][kScanWaves];
+  __shared__ Pair room[2][kScanWaves];
   bool used[4];
   int64_t at;
-  used_of(p, used, at);
-  int64_t mine = 0, others = 0;  // pages in use in earlier blocks, in all
-  for (int b = static_cast<int>(threadIdx.x); b < p.blocks; b += kScanThreads) {
-    others += p.counts[b];
-    mine += b < static_cast<int>(blockIdx.x) ? p.counts[b] : 0;
+  const int64_t c = used_of(p, static_cast<int>(blockIdx.x), used, at);
+  uint32_t mine = 0, others = 0;  // pages in use in earlier blocks, in all
+  if (p.blocks <= kFewBlocks) {
+    for (int b = 0; b < p.blocks; ++b) {
+      bool u[4];
+      int64_t a;
+      const int n = b == static_cast<int>(blockIdx.x) ? static_cast<int>(c) : used_of(p, b, u, a);
+      others += n;
+      mine += b < static_cast<int>(blockIdx.x) ? n : 0;
+    }
+  } else {
+    for (int b = static_cast<int>(threadIdx.x); b < p.blocks; b += kScanThreads) {
+      others += p.counts[b];
+      mine += b < static_cast<int>(blockIdx.x) ? p.counts[b] : 0;
+    }
   }
-  int64_t before, U, here;
-  group_sums<kScanWaves>(mine, room[0], before);
-  group_sums<kScanWaves>(others, room[1], U);
-  const int64_t c = used[0] + used[1] + used[2] + used[3];
-  int64_t used_before = before + group_sums<kScanWaves>(c, room[2], here) - c;
+  Pair sums, here;
+  group_sums<kScanWaves>(Pair{mine, others}, room[0], sums);
+  const int64_t U = sums.b;
+  const Pair own = {static_cast<uint32_t>(c), 0};
+  int64_t used_before = sums.a + static_cast<int64_t>((group_sums<kScanWaves>(own, room[1], here) - own).a);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
+    // the free pages before page U are as many as the moves
+    if (at + e == U) p.counts[p.blocks] = static_cast<int32_t>(U - used_before);
     if (at + e >= p.b.num_pages) break;
     const int64_t free_before = at + e - used_before;
     const int64_t k = used[e] ? U - 1 - used_before : free_before;
@@ -284,10 +371,13 @@ __global__ __launch_bounds__(kScanThreads) void qkn_pages_moves(const MoveParams
     p.moved[at + e] = !moves ? -1 : used[e] ? static_cast<int32_t>(k) : -2;
     used_before += used[e];
   }
+  if (U == static_cast<int64_t>(p.blocks) * kScan && blockIdx.x == 0 && threadIdx.x == 0) p.counts[p.blocks] = 0;  // all in use
 }
 
 __global__ __launch_bounds__(kRowThreads) void qkn_pages_apply(const MoveParams p) {
   const int64_t i = static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x;
+  for (int64_t k = i; k < p.n; k += static_cast<int64_t>(gridDim.x) * kRowThreads)
+    if (k >= p.counts[p.blocks]) p.src[k] = p.dst[k] = -1;
   if (i < p.b.num_pages) {
     const int32_t k = p.moved[i];
     if (k != -2) {  // else the page that moves here writes it
@@ -350,7 +440,7 @@ __global__ __launch_bounds__(kCopyThreads) void qkn_pages_copy_kernel(const Copy
       if (u0 + x * kCopyThreads < static_cast<uint32_t>(c.units)) v[x] = *reinterpret_cast<const U*>(from + off[x]);
 #pragma unroll
     for (int x = 0; x < kCopyEach; ++x)
-      if (u0 + x * kCopyThreads < static_cast<uint32_t>(c.units)) *reinterpret_cast<U*>(to + off[x]) = v[x];
+      if (u0 + x * kCopyThreads < static_cast<uint32_t>(c.units)) __builtin_nontemporal_store(v[x], reinterpret_cast<U*>(to + off[x]));
   }
 }
 
@@ -559,6 +649,9 @@ int qkn_pages_grow(const qkn_pages* book, const int32_t* which, const int32_t* c
   p.pos = pos;
   p.done = done;
   if (!launch(reinterpret_cast<const void*>(qkn_pages_take<false>), 1, 1, kMost, &p, stream)) return QKN_EHIP;
+  if (T > 4 * kMost && (slots || pos) &&
+      !launch(reinterpret_cast<const void*>(qkn_pages_slots), (T + kMany - 1) / kMany, 1, kManyThreads, &p, stream))
+    return QKN_EHIP;
   return launched("pages_grow", 1, kMost);
 }
 
@@ -616,7 +709,7 @@ int qkn_pages_free(const qkn_pages* book, const int32_t* which, int32_t n, void*
 int64_t qkn_pages_compact_workspace_bytes(const qkn_pages* book) {
   if (!book_ok(book)) return QKN_EINVAL;
   const int64_t blocks = (book->num_pages + kScan - 1) / kScan;
-  return 4 * ((blocks ? blocks : 1) + book->num_pages);
+  return 4 * ((blocks ? blocks : 1) + 1 + book->num_pages);
 }
 
 int qkn_pages_compact(const qkn_pages* book, const qkn_pages* out, int32_t* src, int32_t* dst, int32_t n,
@@ -632,7 +725,8 @@ int qkn_pages_compact(const qkn_pages* book, const qkn_pages* out, int32_t* src,
       !workspace || workspace_bytes < need)
     return QKN_EINVAL;
   if (!aligned(workspace, 16)) return QKN_ENOTSUP;
-  const int64_t work = (book->num_pages + entries + kRowThreads - 1) / kRowThreads;
+  int64_t work = (book->num_pages + entries + kRowThreads - 1) / kRowThreads;
+  if (work == 0) work = 1;  // the lists alone
   if (work >= int64_t{1} << 31) return QKN_ENOTSUP;
   Arrays a;
   a.book(*book);
@@ -654,9 +748,9 @@ int qkn_pages_compact(const qkn_pages* book, const qkn_pages* out, int32_t* src,
   p.blocks = static_cast<int32_t>(blocks);
   p.moved = static_cast<int32_t*>(workspace);
   p.counts = p.moved + book->num_pages;
-  if (!launch(reinterpret_cast<const void*>(qkn_pages_count), blocks, 1, kScanThreads, &p, stream) ||
+  if ((blocks > kFewBlocks && !launch(reinterpret_cast<const void*>(qkn_pages_count), blocks, 1, kScanThreads, &p, stream)) ||
       !launch(reinterpret_cast<const void*>(qkn_pages_moves), blocks, 1, kScanThreads, &p, stream) ||
-      (work && !launch(reinterpret_cast<const void*>(qkn_pages_apply), work, 1, kRowThreads, &p, stream)))
+      !launch(reinterpret_cast<const void*>(qkn_pages_apply), work, 1, kRowThreads, &p, stream))
     return QKN_EHIP;
   return launched("pages_compact", work, kRowThreads);
 }

@@ -289,7 +289,7 @@ __global__ __launch_bounds__(64 * kWaves) void qkn_rope(const RopeParams p) {
   const int64_t page = slot >> p.page_shift, row = slot & p.page_mask;
   if constexpr (F == kFp4) {
     if constexpr (V == 8)
-      if (p.cached) store_cache4(of_v ? p.vp : p.kp, of_v ? p.ve : p.ke, page, row, head, a, b, apart, keep, fa, fb);
+      if (__builtin_amdgcn_ballot_w64(keep)) store_cache4(of_v ? p.vp : p.kp, of_v ? p.ve : p.ke, page, row, head, a, b, apart, keep, fa, fb);
   } else if (p.cached && keep) {
     if (of_v) store_cache<V, F>(p.vp, page, row, head, a, b, has_b, scale, fa, fb);
     else store_cache<V, F>(p.kp, page, row, head, a, b, has_b, scale, fa, fb);

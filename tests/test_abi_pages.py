@@ -78,7 +78,7 @@ def test_refusals(dry):
     for other in (dict(num_pages=4095), dict(rows=127), dict(ld_table=63), dict(page_size=32), dict(refs=None), dict(table=None)):
         assert calls(dry, book(), out=book(200, **other))[3] == e
     need = dry.qkn_pages_compact_workspace_bytes(p)
-    assert need == 4 * (4096 + 1) and calls(dry, book(), ws_bytes=need)[3] == DRY
+    assert need == 4 * (4096 + 1 + 1) and calls(dry, book(), ws_bytes=need)[3] == DRY
     assert calls(dry, book(), ws_bytes=need - 1)[3] == e and calls(dry, book(), ws=None)[3] == e
     assert calls(dry, book(), ws=BASE + 150 * MB + 4)[3] == L.QKN_ENOTSUP
 
