@@ -10,10 +10,10 @@
  * An element is a 4-bit E2M1 code: a sign (bit 3) and one of the values 0, 0.5,
  * 1, 1.5, 2, 3, 4, 6 (bits 0 to 2, in this order). 32 consecutive elements of a
  * head's row share an exponent byte E: a code's value is multiplied by
- * 2^(E - 127); E = 255 makes the elements NaN. From E = 2, the least that the
- * quantiser writes, to 252, the most, such values are exact and normal in bf16
- * (beyond: infinite, or so small that a reader may take 0). 17 bytes hold 32
- * elements.
+ * 2^(E - 127); E from 253 on makes the elements NaN (the quantiser writes 255).
+ * From E = 2, the least that the quantiser writes, to 252, the most, such values
+ * are exact and normal in bf16 (below, so small that a reader may take 0). 17
+ * bytes hold 32 elements.
  *
  * The quantiser, for a block whose largest magnitude is A: the exponent is
  *   e = the least with A < 7 * 2^e, within [-125, 125];   E = e + 127,

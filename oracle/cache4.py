@@ -44,7 +44,7 @@ def values(codes, exps):
     code = np.stack([codes & 15, codes >> 4], -1).reshape(*codes.shape[:-1], -1)
     v = np.where(code & 8, -1.0, 1.0) * VALUES[code & 7]
     e = np.repeat(exps, 32, -1).astype(np.float64)
-    return np.where(e == 255, np.nan, v * 2.0 ** (e - 127))
+    return np.where(e >= 253, np.nan, v * 2.0 ** (e - 127))
 
 
 def check_stored(codes, exps, x, error, what):

@@ -8,7 +8,7 @@ namespace attn {
 
 // 32 keys a tile; as many workgroups on a CU as registers and LDS have room for.
 constexpr int occupancy(int dt, int format, int cb) {
-  return cb == 1 ? (dt == 64 || (dt == 128 && format == kFp8) ? 4 : dt == 128 ? 2 : format == kFp4 ? 2 : 1)
+  return cb == 1 ? (dt == 64 || (dt == 128 && format != kBf16) ? 4 : dt == 128 || format == kFp4 ? 2 : 1)
                  : dt == 64 || (dt == 128 && cb == 2) ? 2 : 1;
 }
 template <int DT, int F, int CB, bool SINKS>

@@ -165,7 +165,12 @@ struct Cfg {
   static constexpr int LDS = BUFFERS * BUF * STAGES > JOIN ? BUFFERS * BUF * STAGES : JOIN;
   static_assert(BR % RPL == 0, "whole load instructions");
   static_assert(WAVES == 4, "a wavefront of a workgroup on each SIMD");
-  static constexpr int SLOTS = OCC < 160 * 1024 / LDS ? OCC : 160 * 1024 / LDS;  // workgroups that a CU holds
+  static constexpr int FIT = OCC < 160 * 1024 / LDS ? OCC : 160 * 1024 / LDS;  // workgroups that a CU holds
+  // and that keys are split for. Parts of a 4-bit cache are few steps each, and every part begins with microseconds of
+  // latencies: 64 single tokens over up to 4096 keys, 8 + 2 heads of 128, 18.5 us split for 3, 17.4 for 2; heads of 64 16.0
+  // for 4, 15.4 for 2. Unsplit, more wavefronts are faster: 128 over up to 8192 keys, 8 + 8 heads, 147 us with 3 on a SIMD,
+  // 134 with 4.
+  static constexpr int SLOTS = FP4 && !SHARED && FIT > 2 ? 2 : FIT;
   static_assert(LDS <= 160 * 1024, "LDS");
   static_assert(CH <= 64 && V_LOADS < 64, "loads");
   // Chunk c of row r is stored at c ^ swizzle(r). K: 16 lanes read the same chunk of 16 rows.
@@ -351,7 +356,7 @@ struct Tiles {
       load4(codes, exps, V ? v_off[i] : k_off[i], V ? ve_off[i] : ke_off[i], x.w[i], x.e[i]);
   }
   // Writes such rows as bf16, row row0 of the K (V) tile in buffer `at` on; j is the first one's key. `finite`: 0 in the
-  // place of NaN; true if there was any in the sequence's rows.
+  // place of NaN (rows past the sequence's last hold any bytes); true if there was any in the sequence's rows.
   template <bool V>
   __device__ __forceinline__ bool put(const Codes& x, int row0, int at, bool finite, int32_t j) {
     bool any = false;
@@ -360,7 +365,7 @@ struct Tiles {
       const int r = row0 + i * (64 / C::ROW_LANES) + lane / C::ROW_LANES;
       unsigned char* row = buf + at * C::BUF + (V ? C::V_AT : 0) + r * C::RB;
       const int chunk0 = lane % C::ROW_LANES * C::CODE_WORDS, swizzle = V ? C::swizzle_v(r) : C::swizzle_k(r);
-      const bool nan = x.e[i] == 255;
+      const bool nan = x.e[i] >= quant4::kNan;
       const bool some = __builtin_amdgcn_ballot_w64(nan);
       if (__builtin_expect(some && finite, 0)) any |= __builtin_amdgcn_ballot_w64(nan && j + (r - row0) < kv_len) != 0;
 #pragma unroll
@@ -540,7 +545,8 @@ __device__ __forceinline__ void scores(const Tiles<C>& t, const Rows<C>& w, cons
       if (n < NS * KB) a[n % RING] = t.k_frag(at, n % KB, n / KB);
       f = Tiles<C>::operand(a[i % RING]);
     } else if constexpr (C::FP4) {
-      f = quant4::decode(kr[kb][step / C::CODE_WORDS][step % C::CODE_WORDS], ke[kb][step / C::CODE_WORDS]);
+      const uint32_t e = ke[kb][step / C::CODE_WORDS];
+      f = quant4::decode(kr[kb][step / C::CODE_WORDS][step % C::CODE_WORDS], e >= quant4::kNan ? 255 : e);  // 255: NaN
     } else if constexpr (C::FP8) {
       const u32x4 u = kr[kb][step / 2];
       f = Tiles<C>::widen(i32x2{static_cast<int>(u[2 * (step % 2)]), static_cast<int>(u[2 * (step % 2) + 1])});
@@ -665,7 +671,7 @@ __device__ __forceinline__ void add_infinities(const Tiles<C>& t, Rows<C>& w, in
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         float v;
-        if constexpr (C::FP4) v = exps[d / 32] == 255 ? __builtin_nanf("") : 0.0f;
+        if constexpr (C::FP4) v = exps[d / 32] >= quant4::kNan ? __builtin_nanf("") : 0.0f;
         else if constexpr (C::FP8) v = (row[d + r] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f;
         else v = bf16_lo(reinterpret_cast<const uint16_t*>(row)[d + r]);
         if (__builtin_isfinite(v)) continue;

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kThreads) void qkn_cache4_rows(const LoadParams p) 
     else w = from[0] | from[1] << 8 | from[2] << 16 | static_cast<uint32_t>(from[3]) << 24;
   }
   u32x4 u = __builtin_bit_cast(u32x4, quant4::decode(w, e));
-  if (e == 255) u = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+  if (e >= quant4::kNan) u = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
   uint16_t* y = (s ? p.y[1] : p.y[0]) + t * (s ? p.ld[1] : p.ld[0]) + static_cast<int64_t>(head) * D + c;
   if constexpr (VEC) {
     *reinterpret_cast<u32x4*>(y) = u;

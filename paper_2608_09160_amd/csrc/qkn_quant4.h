@@ -8,6 +8,9 @@ namespace quant4 {
 
 using namespace qkn_block;
 
+// Exponent bytes from here on make a block NaN: the quantiser writes 255; with 253 and 254 a value could be infinite.
+constexpr uint32_t kNan = 253;
+
 // x c + y s, each operation rounded by itself.
 __device__ __forceinline__ float cross(float x, float c, float y, float s) {
 #pragma clang fp contract(off)
@@ -57,7 +60,7 @@ __device__ __forceinline__ uint32_t encode(const float (&f)[8], uint32_t e) {
   return e == 255 ? 0 : u;
 }
 
-// Eight codes times 2^(e - 127) as bf16, exactly. e is neither 255 (the conversion is not asked for NaN) nor 1.
+// Eight codes times 2^(e - 127) as bf16, exactly; e below kNan.
 __device__ __forceinline__ bf16x8 decode(uint32_t w, uint32_t e) {
   const float scale = __builtin_bit_cast(float, e << 23);
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);

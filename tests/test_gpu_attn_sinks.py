@@ -231,6 +231,34 @@ def test_unseen_infinities_and_nan_reach_no_row(fmt, value, hq):
                 assert same.all()
 
 
+@pytest.mark.parametrize("hq", [2, 16, 40, 130])
+@pytest.mark.parametrize("exponent", [0, 1, 252, 253, 254, 255])
+def test_what_lies_behind_a_sequence_in_its_last_page(exponent, hq):
+    """Rows that were never written hold any bytes: exponents whose values are beyond bf16 too."""
+    lens = [(1, 70), (1, 1), (37, 150), (20, 20)]
+    batch = Batch(33, lens, hq, 1, 64, 32)
+    want, want_lse = batch.run(window=40, sinks=3)
+    unused = [np.repeat(e == 255, 16, -1) for _, e in batch.bytes]
+    for (codes, exps), bad in zip(batch.bytes, unused):
+        codes[bad] = np.random.default_rng(1).integers(0, 256, int(bad.sum()))
+        exps[exps == 255] = exponent
+    out, lse = batch.run(window=40, sinks=3)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("hq", [2, 16, 40, 130])
+@pytest.mark.parametrize("exponent", [253, 254, 255])
+@pytest.mark.parametrize("which", [0, 1])
+def test_a_nan_block_is_in_the_rows_that_see_it(which, exponent, hq):
+    n, m, window, sinks = 37, 150, 20, 6
+    for j in (5, m - n - 3, m - 20):
+        batch = Batch(34, [(n, m), (1, 64)], hq, 1, 64, 16)
+        page, row = int(batch.table[0, j // 16]), j % 16
+        batch.bytes[which][1][page, 0, row, 1] = exponent
+        batch.values[which] = O.values(*batch.bytes[which])
+        batch.check(*batch.run(window=window, sinks=sinks), window=window, sinks=sinks)
+
+
 def test_table_entries_and_lengths_outside_their_ranges_stay_inside_the_buffers():
     batch = Batch(16, [(1, 40), (20, 60)], 4, 1, 64)
     batch.table[0, 1], batch.table[1, 2] = -5, 1 << 30

@@ -47,7 +47,7 @@ def test_every_code_under_every_exponent():
     ref = O.values(_bytes(codes)[:, 0, 0], _bytes(exps)[:, 0, 0])
     for got in (k, v):
         assert np.array_equal(_host(got)[2:253], ref[2:253])
-        assert got[255].isnan().all()
+        assert got[253:].isnan().all()
 
 
 @pytest.mark.parametrize("D,pad,shift,kernel", [(128, 0, 0, "rope<8>/fp4"), (32, 0, 0, "rope<8>/fp4"), (96, 0, 0, "rope<8>/fp4"),
