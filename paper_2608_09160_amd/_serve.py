@@ -320,6 +320,8 @@ class PreparedAttn:
         if lse is not None and tuple(lse.shape) != (T, heads):
             raise ValueError(f"lse: expected [{T}, {heads}]")
         limit = 2 ** 31 - 1
+        if not 0 <= sinks <= limit:
+            raise ValueError(f"sinks: expected 0 to {limit}, got {sinks}")
         max_q = min(T, limit) if max_q is None else max_q
         max_kv = min(pages * c.page_size, limit) if max_kv is None else max_kv
         a = QknAttnArgs(pq, ldq, po, ldo, _f32(lse, "lse"), _index(q_start, "q_start", torch.int32, batch + 1),

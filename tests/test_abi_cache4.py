@@ -230,3 +230,15 @@ def test_bindings_checks():
         pools.update(bad)
         with pytest.raises(ValueError):
             S.KVCache4(**pools).struct()
+
+
+@pytest.mark.parametrize("sinks", [-1, 2 ** 31, 2 ** 32])
+def test_first_tokens_that_no_32_bits_hold(sinks, monkeypatch):
+    """Refused, not taken modulo 2^32."""
+    monkeypatch.setattr(S, "_rows", lambda t, what, *a: (BASE, 128, t.shape[0], t.shape[1]))
+    monkeypatch.setattr(S, "_index", lambda t, what, dtype, n: BASE)
+    monkeypatch.setattr(S.KVCache4, "struct", lambda self: cache(64))
+    ints = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="sinks"):
+        S.PreparedAttn(torch.empty(1, 128), S.KVCache4.empty(1, 2, 16, 64, device="cpu"), ints.view(1, 2), ints, ints[:1],
+                       window=4, sinks=sinks, out=torch.empty(1, 128))

@@ -255,3 +255,31 @@ def test_no_tokens_and_no_pages():
     slots = torch.zeros(2, dtype=torch.int64, device=DEV)
     qkn.qkn_rope_cache(None, None, 64, k=qkn.RopeSeg(x), v=x, cache=cache, slots=slots)
     assert all(t.count_nonzero() == 0 for t in qkn.qkn_cache4_load(cache, slots))
+
+
+def test_pages_beyond_32_bits():
+    """A page stride of over 2^31 bytes: written, read back, attended to and copied at its place."""
+    g = torch.Generator().manual_seed(9)
+    D, hk, page, stride = 64, 2, 16, (1 << 31) + (1 << 20)
+    big = torch.empty(3 * stride + (1 << 20), dtype=torch.uint8, device=DEV)
+
+    def pool(at, width):
+        return big[at:].as_strided((4, hk, page, width), (stride, page * width, width, 1))[:3]
+    far = qkn.KVCache4(pool(0, D // 2), pool(1 << 16, D // 2), pool(1 << 17, D // 32), pool(1 << 18, D // 32))
+    near = qkn.KVCache4.empty(3, hk, page, D, DEV)
+    k, v = (_rows(g, 40, hk * D) for _ in range(2))
+    q = _rows(g, 1, 4 * D)
+    slots = torch.arange(40, device=DEV) + 5
+    ints = dict(dtype=torch.int32, device=DEV)
+    outs = []
+    for cache in (far, near):
+        for t in (cache.k, cache.v, cache.k_exp, cache.v_exp):
+            t.zero_()
+        qkn.qkn_rope_cache(None, None, D, k=qkn.RopeSeg(k), v=v, cache=cache, slots=slots)
+        rows = qkn.qkn_cache4_load(cache, slots)
+        out = qkn.qkn_attn(q, cache, torch.tensor([[0, 1, 2]], **ints), torch.tensor([0, 1], **ints), torch.tensor([45], **ints),
+                           window=20, sinks=3)
+        qkn.qkn_pages_copy([cache], torch.tensor([2], **ints), torch.tensor([0], **ints))
+        outs.append([*rows, out, qkn.qkn_cache4_load(cache, torch.arange(48, device=DEV))[0]])
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+    assert torch.equal(outs[0][3][:16], outs[0][3][32:])

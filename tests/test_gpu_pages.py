@@ -342,3 +342,25 @@ def test_empty_calls():
     qkn.qkn_pages_copy([], src, dst)
     b = qkn.PageBook.empty(0, 3, 64, 16, DEV)  # no pages at all
     assert _ints(qkn.qkn_pages_grow(b, _i32([1, 0, 2]))) == [-1, 0, -1]
+
+
+def test_calls_on_a_given_stream():
+    """Each call, and what it allocates, on the stream that it is given."""
+    side = torch.cuda.Stream()
+    b = Both(60, 6, 100, 16)
+    cache, pools = _pools("bf16", 60, 2, 16, 64, "heads first", torch.Generator().manual_seed(2))
+    counts, which, parents, to = _i32([40, 21, 5]), _i32([0, 1, 2]), _i32([0, 1, 1]), _i32([3, 4, 5])
+    src, dst = (torch.empty(30, dtype=torch.int32, device=DEV) for _ in range(2))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):  # another one is current
+        qkn.qkn_pages_grow(b.dev, counts, which, stream=side)
+        qkn.qkn_pages_fork(b.dev, parents, to, [cache], stream=side)
+        qkn.qkn_pages_free(b.dev, which, stream=side)
+        qkn.qkn_pages_compact(b.dev, src, dst, [cache], stream=side)
+        qkn.qkn_pages_copy([cache], src, dst, stream=side)
+    b.ref.grow([40, 21, 5], [0, 1, 2])
+    b.ref.fork([0, 1, 1], [3, 4, 5])
+    b.ref.free([0, 1, 2])
+    want = b.ref.compact(30)
+    b.same()
+    assert [_ints(src), _ints(dst)] == [list(map(int, w)) for w in want]
