@@ -9,7 +9,9 @@ Around the norm, what an attention block needs to serve: rotary positions with
 the write into a paged cache (``csrc/qkn_rope.hip``), attention over that cache
 (``csrc/qkn_attn*``) and low-rank adapters (``csrc/qkn_adapters.hip``), declared
 in ``include/qkn_rope.h``, ``qkn_attn.h``, ``qkn_adapters.h`` and ``qkn_cache.h``;
-``_serve`` is their binding, ``block`` runs them together.
+``_serve`` is their binding, ``block`` runs them together. For long contexts the
+cache may be held in 4 bits (``include/qkn_cache4.h``) and its pages be handed out
+on the device (``include/qkn_pages.h``, binding ``_pages``).
 """
 from ._lib import (QKN_EHIP, QKN_EINVAL, QKN_ENOTSUP, QKN_EOVERLAP, QKN_OK,  # noqa: F401
                    Prepared, PreparedApply, PreparedPartial, QknError, Seg, load, qkn_apply, qkn_full, qkn_fused_shard,

@@ -1,5 +1,5 @@
-"""ctypes binding of the attention block's entry points (include/qkn_rope.h, qkn_attn.h, qkn_adapters.h, qkn_cache.h): argument marshalling
-only, as in ``_lib``.
+"""ctypes binding of the attention block's entry points (include/qkn_rope.h, qkn_attn.h, qkn_adapters.h, qkn_cache.h, qkn_cache4.h):
+argument marshalling only, as in ``_lib``.
 
 Row tensors are 2-D with a contiguous last dimension and any row stride; heads follow each other in a row, as
 the projection writes them. Each operator has a ``Prepared...`` class, whose arguments are checked and marshalled

@@ -27,6 +27,22 @@
 //           wavefronts' results are joined at the end (few rows: bytes bound it). No other wavefront wants its K rows,
 //           and a row is an operand as it is: they go to registers, LDS has V only, and with half the LDS a CU holds
 //           twice the wavefronts, so twice the bytes are on their way.
+// 4-bit caches. A code times its block's power of two is a bf16 value, and one conversion gives two of them. Codes and
+// exponents go to registers a tile ahead. K's rows of few-row tiles stay there and are widened as operands: a lane's 16 bytes
+// are 32 elements of one exponent. V's, and both tiles of SHARED workgroups, are written to LDS as bf16 (each wavefront a
+// quarter of a SHARED tile), so all behind it is the bf16 kernel; exponents belong to keys, so that codes in LDS would need
+// weights of their own for every 32 elements. The loads go out whether a tile is wanted or not (an empty descriptor reads no
+// memory): in a branch the compiler waited for all of them behind it, and nothing was ahead any more (64 single tokens over
+// up to 4096 keys 23.2 us, then 18.8). Pages are looked up once a tile, and what is rare (a mask, a NaN, a raised bound, the
+// next 64 pages) lies outside the loop's straight line: 16.9 and 16.7 us. Slower: two tiles ahead (by 1.7 us, with 176
+// registers for 136), 64 keys a wavefront (19.1), addresses of 64 pages in registers (18.3), one wavefront that finds the
+// workgroup's part for all four (by 0.2).
+//
+// First keys beside a window (SINKS). The list of a row tile's key steps is those of the first keys, as far as they lie before
+// the window's, then the window's; everything else counts positions in that list. Pages are held ahead in the order of the
+// list. A masked tile asks two comparisons for one, and 64 more keys a row tile: 12 windowed chunks of up to 512 tokens take
+// 29.2 us with 64 first keys, 25.8 without. Kernels of their own, so that calls without first keys keep theirs.
+//
 // Over workgroups the keys are split further where rows alone do not fill the chip (`schedule`); qkn_attn_join adds the
 // parts in a fixed order.
 //
@@ -41,6 +57,11 @@
 // 1024, 16 + 2 heads of 64, 25.8 us) too: a wavefront's 16 rows and 64 keys take 256 cycles of products and 620 of
 // other vector instructions; 560 workgroups make three wavefronts on some SIMDs, whose up to 3 x 18 such steps are the
 // call's 49 k cycles.
+// Over 4 bits: 64 single tokens over up to 4096 keys, 37 MB, 16.8 us, and 16 over up to 32768, 84 MB, 23.6 us (the join 4.0 and
+// 4.4 of them): a wavefront's 12,600 turns of four cycles are 4,100 instructions issued (1,780 vector, 2,110 scalar) and half
+// waiting, for lengths, pages and the first tile one after the other in the first 4 us, then for the tiles. A prompt of 8192
+// tokens 309 us, 0.89 Pflop/s, bf16's cycles and a tenth for the widening; 128 single tokens over up to 8192 keys of 8 + 8
+// heads, not split, 134 us (bf16 414).
 // Slower: the wavefronts in two groups that take turns at products and softmax (288 to 309 us), 64 rows a wavefront with
 // one tile's softmax between another's products (322), wave priorities by phase and operands fetched 1 to 10 products ahead
 // (within 4 %).

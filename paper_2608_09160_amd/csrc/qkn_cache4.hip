@@ -2,7 +2,8 @@
 // attention in qkn_attn*.
 //
 // Bytes bound it: 17/32 of a byte in and 2 out for an element. A lane takes 8 elements, one word of codes, and stores
-// one 16-byte vector; four lanes share an exponent.
+// one 16-byte vector; four lanes share an exponent. 8192 tokens of 4 + 4 heads of 128, 21 MB, 7.1 us, 64 tokens 2.7: a launch
+// and two trips to memory, slot and codes. Four such units a lane were no faster (7.4 and 3.7 us).
 
 #include <string.h>
 

@@ -2,7 +2,10 @@
 //
 // The book's calls are integer work on small arrays, each a chain of latencies: taking pages is one workgroup, so that
 // ranks among the free pages and among the rows' needs need no second launch; the rest has a workgroup for a row or for
-// 4096 pages. Copies are bound by bytes.
+// 4096 pages. Sums over lanes go by DPP: through LDS, in 64 bits, 8 rows that are emptied and grown again by up to 2048
+// tokens each, in a book of 8192 pages, took 15.3 us for 12.7 (2.7 emptying, 5.6 taking, 4.7 the slots, which one workgroup
+// made 17.8). 64 rows emptied and forked from 16: 2.8, 8.0 taking, 3.0 sharing. The moves of 4096 pages: 4.7 and 4.7 in two
+// launches (4.6, 7.1 and 4.6 with the counts in a launch of their own). Copies are bound by bytes.
 
 #include <string.h>
 
@@ -416,9 +419,9 @@ struct CopyParams {
   int32_t chunks;
 };
 
-// EACH: vectors of a thread. Pages are read as they are (forks read the same one several times) and written past the
-// caches: 980 of 2048 pages of 32 KiB in four layers, 258 MB, 51.7 us with the list's launches (5.8 TB/s the copy alone),
-// 58 with stores into the caches; 64 forks of 16 pages 13.8 us with loads past them, 9.6 without.
+// EACH: vectors of a thread. Pages are read as they are (forks read the same one several times: 64 of 16 pages 9.6 us,
+// 13.8 with loads past the caches) and written past the caches (980 of 2048 pages of 32 KiB in four layers, 258 MB, with the
+// list's launches 59.4 us, 66.3 with stores into them). A workgroup for each pair: 51.7 of those 59.4, 5.7 TB/s the copy.
 template <class U, int EACH>
 __global__ __launch_bounds__(kCopyThreads) void qkn_pages_copy_kernel(const CopyParams p) {
   const CopyPool& c = p.pool[blockIdx.y];
