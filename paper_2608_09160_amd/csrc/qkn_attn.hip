@@ -88,6 +88,13 @@ constexpr int64_t kJoinFew = 2048;  // rows
 // Key steps of a part, at least (few rows: 128 keys each, many: 64): a part costs a workgroup's start and a share of the
 // join (4 single tokens over up to 500 keys, D 128: 9.4 us whole, 11.6 in parts of two steps).
 constexpr int kMinPart = 4;
+// Such parts of keys from which a 4-bit cache's are also split where that only makes sequences of unequal lengths even, or
+// fills a chip that the whole tiles fill by half: as many workgroups as the chip holds (single tokens, heads of 128, us
+// whole and split: 32 over up to 16384 keys, 32 + 8 heads 133 and 72.6, 48 162 and 98.9, over 16384 each 175 and 162; 64
+// over up to 4096, 16 + 8 heads 47.4 and 43.0; 32 of 4 tokens over up to 8192, 64 + 8 heads 76.3 and 51.8). Equal lengths
+// can lose (64 over 8192 each, 16 + 8 heads 104 and 110; heads of 256, 32 over 4096 each, 64 + 8 heads 60.9 and 65.0), and
+// so do short ones (64 over 2048 each, 8 + 8 heads 31.6 and 36.1).
+constexpr int64_t kLongParts = 8;
 // Pairs of 64 rows and 64 keys up to which many-row launches take 64 rows to a workgroup (16 + 4 heads of 128, us with 64
 // and with 128 rows: prompts of 256 tokens 9.6 and 12.2, 1024 21.7 and 26.6, 2048 39.1 and 49.7, 8192 344 and 277; 128
 // tokens behind 8064 24.9 and 26.7, 512 behind 7680 54.1 and 49.9; 16 + 2 heads of 64, 12 chunks of up to 512 tokens,
@@ -182,6 +189,14 @@ Plan plan_with(const qkn_attn_args& a, const Source& c, const Variant& v) {
     // the workgroups that take turns on the chip, or as many as the keys can use
     const int64_t most = pl.items * ((a.max_kv + part - 1) / part);
     pl.items = slots < most ? slots : most;
+  } else if (c.format == kFp4 && a.batch) {
+    const int64_t full = int64_t{pl.v.fit} * kCus / c.n_kv, keys = a.window && a.window < a.max_kv ? a.window : a.max_kv;
+    // row tiles of max_q tokens a sequence; sequences may have more, which the workgroups have to suffice for
+    const int64_t each = ((a.max_q < 1 ? 1 : a.max_q) * group + pl.v.rows - 1) / pl.v.rows * a.batch;
+    pl.split = 2 * (each < pl.items ? each : pl.items) <= full && keys >= kLongParts * part;
+    if (pl.split && pl.items < full) pl.items = full;
+  }
+  if (pl.split) {
     pl.ml_bytes = pl.items * c.n_kv * pl.v.rows * 8;
     pl.o_bytes = pl.items * c.n_kv * pl.v.rows * 4 * int64_t{c.head_dim};
     pl.ws_bytes = pl.o_bytes + pl.ml_bytes + a.T * a.n_q * 8;
@@ -204,19 +219,24 @@ Plan plan_of(const qkn_attn_args& a, int32_t sinks, const Source& c, int64_t* wo
   const int dt = c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256;
   const int64_t group = a.n_q / c.n_kv, rows = (a.max_q < 1 ? 1 : a.max_q) * group;
   const bool few = rows <= (dt == 256 ? 32 : 64);
+  // the mask chooses kernels and splits, not the workspace: one serves a model's layers with and without a window
+  qkn_attn_args whole = a;
+  whole.window = 0;
   if (few) {
-    const Plan pl = plan_with(a, c, few_rows_of(c, sinks, dt, static_cast<int>(rows)));
-    if (workspace_bytes) *workspace_bytes = pl.ws_bytes;
-    return pl;
+    const Variant v = few_rows_of(c, sinks, dt, static_cast<int>(rows));
+    if (workspace_bytes) *workspace_bytes = plan_with(whole, c, v).ws_bytes;
+    return plan_with(a, c, v);
   }
   // keys that a row sees, about, and pairs of 64 rows and 64 keys in all
   int64_t keys = a.max_kv - (a.causal ? (a.max_q < a.max_kv ? a.max_q : a.max_kv) / 2 : 0);
   if (a.window && int64_t{a.window} + sinks < keys) keys = int64_t{a.window} + sinks;
   const int64_t pairs = (a.T * group + 63) / 64 * c.n_kv * ((keys + 63) / 64);
-  const Plan small = plan_with(a, c, many_rows_of(c, sinks, dt, true)), large = plan_with(a, c, many_rows_of(c, sinks, dt, false));
-  // the mask chooses between them, not the workspace: one serves a model's layers with and without a window
-  if (workspace_bytes) *workspace_bytes = small.ws_bytes > large.ws_bytes ? small.ws_bytes : large.ws_bytes;
-  return pairs <= kSmallPairs ? small : large;
+  const Variant small = many_rows_of(c, sinks, dt, true), large = many_rows_of(c, sinks, dt, false);
+  if (workspace_bytes) {
+    const int64_t s = plan_with(whole, c, small).ws_bytes, l = plan_with(whole, c, large).ws_bytes;
+    *workspace_bytes = s > l ? s : l;
+  }
+  return plan_with(a, c, pairs <= kSmallPairs ? small : large);
 }
 
 int attn_impl(const qkn_attn_args* args, int32_t sinks, const Source* cache, void* workspace, int64_t workspace_bytes,

@@ -121,7 +121,8 @@ struct Params {
 // A kernel and what its launch has to know.
 struct Variant {
   const void* fn;
-  int rows, step, threads, lds, slots;  // rows of a workgroup; keys that it takes at a time; workgroups of a CU
+  int rows, step, threads, lds;  // rows of a workgroup; keys that it takes at a time
+  int slots, fit;                // workgroups of a CU that keys are split for, and that it holds
   const char* name;
 };
 
@@ -1167,7 +1168,8 @@ __global__ __launch_bounds__(64 * C::WAVES, C::OCC) void qkn_attn_kernel(const P
 
 template <class C>
 Variant variant(const char* name) {
-  return Variant{reinterpret_cast<const void*>(&qkn_attn_kernel<C>), C::BM, C::STEP, 64 * C::WAVES, C::LDS, C::SLOTS, name};
+  return Variant{reinterpret_cast<const void*>(&qkn_attn_kernel<C>), C::BM, C::STEP, 64 * C::WAVES, C::LDS, C::SLOTS,
+                 C::FIT, name};
 }
 
 // A kernel for sequences of up to `rows` rows, and one for more. dt: 64, 128 or 256.

@@ -120,6 +120,16 @@ def test_workspace(dry):
     need = dry.qkn_attn4_workspace_bytes(ctypes.byref(a), ctypes.byref(c))
     assert need > 0 and attn4(dry, ws_bytes=need) == DRY and attn4(dry, ws_bytes=need - 1) == L.QKN_EINVAL
     assert attn4(dry, args(window=64), sinks=9, ws_bytes=need) == DRY
+    # a layer's without a window is enough for its windows, whichever tiles are split
+    for T, batch, max_q, n_kv in ((64, 64, 1, 8), (40, 40, 1, 8), (400, 100, 4, 8), (1000, 64, 60, 1), (9000, 2, 4096, 1)):
+        for max_kv in (1, 511, 2048, 4095, 4096, 100000):
+            c = cache(n_kv=n_kv, num_pages=8, k_page=16 * 64 * n_kv, v_page=16 * 64 * n_kv, ke_page=64 * n_kv, ve_page=64 * n_kv)
+            whole = args(T=T, batch=batch, max_q=max_q, max_kv=max_kv)
+            need = dry.qkn_attn4_workspace_bytes(ctypes.byref(whole), ctypes.byref(c))
+            for window in (0, 1, 4095, 4096, 1 << 20):
+                a = args(T=T, batch=batch, max_q=max_q, max_kv=max_kv, window=window)
+                assert dry.qkn_attn4_workspace_bytes(ctypes.byref(a), ctypes.byref(c)) == need
+                assert attn4(dry, a, c, ws_bytes=need) == DRY
     assert dry.qkn_attn4_workspace_bytes(None, ctypes.byref(c)) == L.QKN_EINVAL
     assert dry.qkn_attn4_workspace_bytes(ctypes.byref(a), None) == L.QKN_EINVAL
 
