@@ -108,10 +108,10 @@ int qkn_pages_compact(const qkn_pages* book, const qkn_pages* out, int32_t* src,
 
 /*
  * Copies page src[i] to page dst[i], i < n, K and V (and exponents), in each of
- * the `count` caches (an array on the host: the layers'). Pairs that are equal, or of which one is
- * outside [0, num_pages), are passed over. What a page holds that is a pair's dst
- * and another pair's src or dst is undefined. Caches may differ in sizes and
- * format; scales of FP8 caches are per head and stay.
+ * the `count` caches (an array on the host: the layers'). Pairs that are equal, or
+ * of which one is outside [0, num_pages), are passed over. What a page holds that
+ * is a pair's dst and another pair's src or dst is undefined. Caches may differ in
+ * sizes and format; scales of FP8 caches are per head and stay.
  */
 int qkn_pages_copy(const qkn_cache* caches, int32_t count, const int32_t* src, const int32_t* dst, int32_t n,
                    void* stream);

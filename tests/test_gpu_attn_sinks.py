@@ -164,15 +164,24 @@ def test_single_tokens_with_split_keys(window, sinks, hq, hk, fmt):
 
 
 @pytest.mark.parametrize("window,sinks", [(0, 0), (4100, 3), (50, 4)])
-@pytest.mark.parametrize("hq,hk,D,most", [(8, 8, 64, 5000), (16, 8, 128, 4500), (8, 8, 256, 2100), (40, 8, 128, 4096)])
+@pytest.mark.parametrize("hq,hk,D,most", [(8, 8, 64, 5000), (16, 8, 128, 4500), (8, 8, 256, 4100), (40, 8, 128, 4096)])
 def test_many_sequences_of_unequal_lengths(hq, hk, D, most, window, sinks):
     """More tiles than fill half the chip's places with few workgroups to a CU, split to make unequal sequences even; also
     where max_q says less than the sequences have."""
-    lens = [(1 + b % 3, (b * 37) % 150) for b in range(40)]
-    lens[0], lens[3], lens[17], lens[39] = (3, most), (0, 0), (1, 2077), (2, 1024)
+    lens = [(1 + b % 3, (b * 37) % 150) for b in range(30 if D == 256 else 40)]
+    lens[0], lens[3], lens[17], lens[-1] = (3, most), (0, 0), (1, 2077), (2, 1024)
     batch = Batch(most + hq, lens, hq, hk, D)
     for max_q in (3, 1):
         batch.check(*batch.run(window=window, sinks=sinks, max_q=max_q), window=window, sinks=sinks, heads=[0, hq - 1])
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (2500, 3), (50, 4)])
+def test_many_chunks_of_unequal_lengths(window, sinks):
+    """As above, of more rows."""
+    lens = [(64 - b % 5, 64 + 9 * b) for b in range(16)]
+    lens[2], lens[15] = (60, 3001), (61, 2048)
+    batch = Batch(window, lens, 16, 4, 128)
+    batch.check(*batch.run(window=window, sinks=sinks), window=window, sinks=sinks, heads=[0, 6, 15])
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "fp4"])
