@@ -16,11 +16,15 @@
 // A 4-bit cache's blocks are four lanes' groups (where pairs are apart) or two lanes' both groups: the largest magnitude
 // crosses lanes by DPP, as integers, and the exponent is a carry from the mantissa. Rows that no vector fits, and heads that
 // do not put a block on neighbouring lanes, take half a wavefront for a block of 32. 8192 tokens of 16 + 4 + 4 heads, 88 MB,
-// 24.4 us: 354 vector instructions a wavefront, issued for 14 of them; two tokens a wavefront, which share gamma, 25.4.
-// Measured: 8192 tokens of 16 + 4 + 4 heads of 128 with the norm, bf16 cache, 105 MB: 24.6 us, 4.3 TB/s; 32768 tokens of
-// 16 + 2 + 2 heads into an FP8 cache, 337 MB: 71 us, 4.7 TB/s; a copy of as many bytes reaches 5 to 5.9. 64 tokens: 5.1 us, a
-// launch and one chain of latencies (position -> angles). Element by element (V = 1) 8192 tokens of 16 + 4 + 4 heads of 50, 41
-// MB, take 37.5 us; of 48, in vectors, 12.8.
+// 23.0 us, half of it the issue of vector instructions; two tokens a wavefront, which share gamma, were slower (25.4 for
+// 24.4 at that time).
+// Instructions count beside the bytes, so what would only move registers is not there: a kernel for each layout of pairs,
+// rows and slots addressed for all lanes at once, and lanes without gamma multiplied by 1 (16 + 4 + 4 heads over 4 bits, 351
+// vector instructions for 562 in the code, 24.4 -> 23.0 us; the cases below 24.5 -> 23.2, 70.7 -> 70.2, 5.4 -> 4.5).
+// Measured: 8192 tokens of 16 + 4 + 4 heads of 128 with the norm, bf16 cache, 105 MB: 23.2 us, 4.5 TB/s; 32768 tokens of
+// 16 + 2 + 2 heads into an FP8 cache, 337 MB: 70 us, 4.8 TB/s; a copy of as many bytes reaches 5 to 5.9. 64 tokens: 4.5 us, a
+// launch and one chain of latencies (position -> angles). Element by element (V = 1) 8192 tokens of 16 + 4 + 4 heads of 50,
+// 41 MB, take 37.5 us; of 48, in vectors, 12.8.
 
 #include <string.h>
 
@@ -75,8 +79,12 @@ struct RopeParams {
 constexpr int kRanks = 4;
 __device__ __forceinline__ void load_ranks(const float* __restrict__ partials, int64_t t, int64_t T, int tp, int r0,
                                            float (&v)[kRanks]) {
+  const float* at = partials + (r0 < tp ? r0 : tp - 1) * T + t;
 #pragma unroll
-  for (int i = 0; i < kRanks; ++i) v[i] = partials[(r0 + i < tp ? r0 + i : tp - 1) * T + t];
+  for (int i = 0; i < kRanks; ++i) {
+    v[i] = *at;
+    at += r0 + i + 1 < tp ? T : 0;
+  }
 }
 // Sum over the ranks, ascending, as Phase B adds them; `v`: the first ones, asked for before.
 __device__ __forceinline__ float rank_sum(const float* __restrict__ partials, int64_t t, int64_t T, int tp,
@@ -154,8 +162,8 @@ __device__ __forceinline__ void store_cache(const PoolDev& pool, int64_t page, i
 // One unit into a 4-bit cache: a block's 32 elements are the groups a (and the groups b) of four lanes where pairs are
 // apart, else both groups of two. Units begin at even lanes (of fours where pairs are apart: head and rotated part are
 // multiples of 64 there), so the lanes of a block are neighbours in one wavefront, all of them running.
-__device__ __forceinline__ void store_cache4(const PoolDev& codes, const PoolDev& exps, int64_t page, int64_t row, int head,
-                                             int a, int b, bool apart, bool keep, const float (&fa)[8], const float (&fb)[8]) {
+__device__ __forceinline__ void store_cache4(uint8_t* p, uint8_t* q, int a, int b, bool apart, bool keep, const float (&fa)[8],
+                                             const float (&fb)[8]) {
   uint32_t ma = quant4::magnitude(fa), mb = quant4::magnitude(fb);
   if (!apart) ma = mb = ma > mb ? ma : mb;
   ma = quant4::max_of_2(ma);
@@ -164,8 +172,6 @@ __device__ __forceinline__ void store_cache4(const PoolDev& codes, const PoolDev
   const uint32_t ea = quant4::exponent(apart ? ma4 : ma), eb = quant4::exponent(apart ? mb4 : mb);
   const uint32_t ca = quant4::encode(fa, ea), cb = quant4::encode(fb, eb);
   if (!keep) return;
-  uint8_t* p = static_cast<uint8_t*>(codes.base) + page * codes.page + head * codes.head + row * codes.token;
-  uint8_t* q = static_cast<uint8_t*>(exps.base) + page * exps.page + head * exps.head + row * exps.token;
   *reinterpret_cast<uint32_t*>(p + a / 2) = ca;
   *reinterpret_cast<uint32_t*>(p + b / 2) = cb;
   if (a % 32 == 0) q[a / 32] = static_cast<uint8_t>(ea);
@@ -182,7 +188,16 @@ __device__ __forceinline__ float cross(float x, float c, float y, float s) {
   }
 }
 
-template <int V, int F>
+// What lanes without gamma multiply by, and what is read for angles where there are none.
+__device__ const float kOnes[16] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f,
+                                    1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
+
+// A pointer to global memory: chosen among parameters and kOnes it would be one to any memory, whose loads are slower.
+typedef const __attribute__((address_space(1))) float* GlobalFloats;
+__device__ __forceinline__ GlobalFloats in_global(const float* p) { return (GlobalFloats)p; }
+
+// INTER: pairs are neighbours (V = 1: either, at run time).
+template <int V, int F, bool INTER>
 __global__ __launch_bounds__(64 * kWaves) void qkn_rope(const RopeParams p) {
   const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + (threadIdx.x >> 6));
   const uint32_t t32 = div(wave, p.parts);
@@ -195,19 +210,14 @@ __global__ __launch_bounds__(64 * kWaves) void qkn_rope(const RopeParams p) {
   const int head = static_cast<int>(div(static_cast<uint32_t>(in_seg), p.per_head));
   const int uh = in_seg - head * static_cast<int>(p.per_head.d);
   const bool turns = !of_v && uh < p.turn_units;
-  const bool apart = turns && !p.interleaved;  // a pair's elements are rot / 2 apart
+  const bool apart = turns && !(V > 1 ? INTER : p.interleaved != 0);  // a pair's elements are rot / 2 apart
   const int a = apart ? uh * V : 2 * uh * V;
   const int b = apart ? a + p.half : a + V;
   const bool has_b = V > 1 || b < p.D;  // an odd head ends in half a unit
   if (u >= p.units) return;             // lanes share nothing from here on
 
-  float fa[V], fb[V];
-  const uint16_t* x = (of_q ? p.q.x + t * p.q.ldx : of_v ? p.v + t * p.ldv : p.k.x + t * p.k.ldx) + head * p.D;
-  load_group<V>(x + a, fa);
-  load_group<V>(x + (has_b ? b : a), fb);
-
   // What the wavefront has in common, and what every lane needs next: all of it asked for before any of it is used, by
-  // all lanes alike (V's units, which need no gamma and no angle, read the first ones), so that the waits are one.
+  // all lanes alike (lanes without gamma read ones, those that do not turn the first angles), so that the waits are one.
   int32_t at = 0;
   int64_t slot = -1;
   float scale = 1.0f;
@@ -222,56 +232,49 @@ __global__ __launch_bounds__(64 * kWaves) void qkn_rope(const RopeParams p) {
   }
   if (p.q.w) load_ranks(p.q.partials, t, p.T, p.tp, 0, ranks_q);
   if (p.k.w) load_ranks(p.k.partials, t, p.T, p.tp, 0, ranks_k);
+
+  float fa[V], fb[V];
+  // the token's rows are the same for all lanes
+  const uint16_t *xq = p.q.x + t * p.q.ldx, *xk = p.k.x + t * p.k.ldx, *xv = p.v + t * p.ldv;
+  const uint16_t* x = (of_q ? xq : of_v ? xv : xk) + head * p.D;
+  load_group<V>(x + a, fa);
+  load_group<V>(x + (has_b ? b : a), fb);
   const float* w = of_q ? p.q.w : of_v ? nullptr : p.k.w;
   float wa[V], wb[V], cs[V][2];
-  if (p.q.w || p.k.w) {
-    const float* any = p.q.w ? p.q.w : p.k.w;
-    const float* w1 = w ? w + head * p.D + a : any;
-    const float* w2 = w && has_b ? w + head * p.D + b : any;
+  const GlobalFloats w1 = in_global(w ? w + head * p.D + a : kOnes), w2 = in_global(w && has_b ? w + head * p.D + b : kOnes);
 #pragma unroll
-    for (int e = 0; e < V; ++e) wa[e] = w1[e];
+  for (int e = 0; e < V; ++e) wa[e] = w1[e];
 #pragma unroll
-    for (int e = 0; e < V; ++e) wb[e] = w2[e];
-  }
-  const bool inside = at >= 0 && at < p.n_pos;  // or nothing turns
-  if (p.half && inside) {
-    const float* row = p.table + 2 * (static_cast<int64_t>(at) * p.half + (turns ? uh * V : 0));
+  for (int e = 0; e < V; ++e) wb[e] = w2[e];
+  const bool inside = at >= 0 && at < p.n_pos, angles = p.half && inside;  // or nothing turns
+  const GlobalFloats row = in_global(angles ? p.table + 2 * (static_cast<int64_t>(at) * p.half) : kOnes) +
+                           (angles && turns ? 2 * uh * V : 0);
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      cs[e][0] = row[2 * e];
-      cs[e][1] = row[2 * e + 1];
-    }
+  for (int e = 0; e < V; ++e) {
+    cs[e][0] = row[2 * e];
+    cs[e][1] = row[2 * e + 1];
   }
 
   float inv_q = 1.0f, inv_k = 1.0f;
   if (p.q.w) inv_q = __builtin_amdgcn_rsqf(__builtin_fmaf(rank_sum(p.q.partials, t, p.T, p.tp, ranks_q), p.q.rcp_d, p.eps));
   if (p.k.w) inv_k = __builtin_amdgcn_rsqf(__builtin_fmaf(rank_sum(p.k.partials, t, p.T, p.tp, ranks_k), p.k.rcp_d, p.eps));
 
-  if (w) {
-    const float inv = of_q ? inv_q : inv_k;
+  const float inv = of_q ? inv_q : of_v ? 1.0f : inv_k;
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      fa[e] = fa[e] * wa[e] * inv;
-      fb[e] = fb[e] * wb[e] * inv;
-    }
+  for (int e = 0; e < V; ++e) {
+    fa[e] = fa[e] * wa[e] * inv;
+    fb[e] = fb[e] * wb[e] * inv;
   }
-  if (!inside) {
-    if (turns) {
+  if (turns) {
+    if constexpr (V > 1 && INTER) {  // pairs (0, 1), (2, 3), ... of group a, then of group b
 #pragma unroll
-      for (int e = 0; e < V; ++e) fa[e] = fb[e] = __builtin_nanf("");
-    }
-  } else if (turns) {
-    if (V > 1 && p.interleaved) {  // pairs (0, 1), (2, 3), ... of group a, then of group b
-      if constexpr (V > 1) {
-#pragma unroll
-        for (int e = 0; e < V; e += 2) {
-          const float c0 = cs[e / 2][0], s0 = cs[e / 2][1], c1 = cs[V / 2 + e / 2][0], s1 = cs[V / 2 + e / 2][1];
-          const float x0 = fa[e], x1 = fa[e + 1], y0 = fb[e], y1 = fb[e + 1];
-          fa[e] = cross<F == kFp4>(x0, c0, -x1, s0);
-          fa[e + 1] = cross<F == kFp4>(x1, c0, x0, s0);
-          fb[e] = cross<F == kFp4>(y0, c1, -y1, s1);
-          fb[e + 1] = cross<F == kFp4>(y1, c1, y0, s1);
-        }
+      for (int e = 0; e < V; e += 2) {
+        const float c0 = cs[e / 2][0], s0 = cs[e / 2][1], c1 = cs[V / 2 + e / 2][0], s1 = cs[V / 2 + e / 2][1];
+        const float x0 = fa[e], x1 = fa[e + 1], y0 = fb[e], y1 = fb[e + 1];
+        fa[e] = cross<F == kFp4>(x0, c0, -x1, s0);
+        fa[e + 1] = cross<F == kFp4>(x1, c0, x0, s0);
+        fb[e] = cross<F == kFp4>(y0, c1, -y1, s1);
+        fb[e + 1] = cross<F == kFp4>(y1, c1, y0, s1);
       }
     } else {
 #pragma unroll
@@ -281,22 +284,33 @@ __global__ __launch_bounds__(64 * kWaves) void qkn_rope(const RopeParams p) {
         fb[e] = cross<F == kFp4>(xb, cs[e][0], xa, cs[e][1]);
       }
     }
+    if (__builtin_expect(!inside, 0)) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) fa[e] = fb[e] = __builtin_nanf("");
+    }
   }
 
-  uint16_t* y = of_q ? p.q.y : of_v ? nullptr : p.k.y;
-  if (y) {
-    y += t * (of_q ? p.q.ldy : p.k.ldy) + head * p.D;
+  if (of_q ? p.q.y != nullptr : !of_v && p.k.y) {
+    uint16_t *yq = p.q.y + t * p.q.ldy, *yk = p.k.y + t * p.k.ldy;
+    uint16_t* y = (of_q ? yq : yk) + head * p.D;
     store_bf16<V>(y + a, fa);
     if (has_b) store_bf16<V>(y + b, fb);
   }
   const bool keep = !of_q && slot >= 0 && slot < p.n_slots;
-  const int64_t page = slot >> p.page_shift, row = slot & p.page_mask;
+  const int64_t page = slot >> p.page_shift, in_page = slot & p.page_mask;
   if constexpr (F == kFp4) {
     if constexpr (V == 8)
-      if (__builtin_amdgcn_ballot_w64(keep)) store_cache4(of_v ? p.vp : p.kp, of_v ? p.ve : p.ke, page, row, head, a, b, apart, keep, fa, fb);
+      if (__builtin_amdgcn_ballot_w64(keep)) {
+        const auto at_row = [&](const PoolDev& pool) {
+          return static_cast<uint8_t*>(pool.base) + page * pool.page + in_page * pool.token;
+        };
+        uint8_t *kc = at_row(p.kp), *vc = at_row(p.vp), *ke = at_row(p.ke), *ve = at_row(p.ve);
+        store_cache4((of_v ? vc : kc) + head * (of_v ? p.vp.head : p.kp.head),
+                     (of_v ? ve : ke) + head * (of_v ? p.ve.head : p.ke.head), a, b, apart, keep, fa, fb);
+      }
   } else if (p.cached && keep) {
-    if (of_v) store_cache<V, F>(p.vp, page, row, head, a, b, has_b, scale, fa, fb);
-    else store_cache<V, F>(p.kp, page, row, head, a, b, has_b, scale, fa, fb);
+    if (of_v) store_cache<V, F>(p.vp, page, in_page, head, a, b, has_b, scale, fa, fb);
+    else store_cache<V, F>(p.kp, page, in_page, head, a, b, has_b, scale, fa, fb);
   }
 }
 
@@ -582,8 +596,15 @@ int rope_impl(const qkn_rope_seg* q, const qkn_rope_seg* k, const uint16_t* v, i
       return QKN_EHIP;
     p.cached = 0;  // the rest writes rows only
   }
-  const auto kernel = vec ? (f == kFp4 ? qkn_rope<8, kFp4> : f == kFp8 ? qkn_rope<8, kFp8> : qkn_rope<8, kBf16>)
-                          : (f == kFp4 ? qkn_rope<1, kFp4> : f == kFp8 ? qkn_rope<1, kFp8> : qkn_rope<1, kBf16>);
+  const auto kernel = !vec            ? (f == kFp4   ? qkn_rope<1, kFp4, false>
+                                         : f == kFp8 ? qkn_rope<1, kFp8, false>
+                                                     : qkn_rope<1, kBf16, false>)
+                      : p.interleaved ? (f == kFp4   ? qkn_rope<8, kFp4, true>
+                                         : f == kFp8 ? qkn_rope<8, kFp8, true>
+                                                     : qkn_rope<8, kBf16, true>)
+                                      : (f == kFp4   ? qkn_rope<8, kFp4, false>
+                                         : f == kFp8 ? qkn_rope<8, kFp8, false>
+                                                     : qkn_rope<8, kBf16, false>);
   const void* fn = reinterpret_cast<const void*>(kernel);
   void* args[] = {&p};
   if (all && hipLaunchKernel(fn, dim3(static_cast<unsigned>(grid)), dim3(64 * kWaves), args, 0, st) != hipSuccess)
