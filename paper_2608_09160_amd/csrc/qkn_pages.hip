@@ -2,10 +2,13 @@
 //
 // The book's calls are integer work on small arrays, each a chain of latencies: taking pages is one workgroup, so that
 // ranks among the free pages and among the rows' needs need no second launch; the rest has a workgroup for a row or for
-// 4096 pages. Sums over lanes go by DPP: through LDS, in 64 bits, 8 rows that are emptied and grown again by up to 2048
-// tokens each, in a book of 8192 pages, took 15.3 us for 12.7 (2.7 emptying, 5.6 taking, 4.7 the slots, which one workgroup
-// made 17.8). 64 rows emptied and forked from 16: 2.8, 8.0 taking, 3.0 sharing. The moves of 4096 pages: 4.7 and 4.7 in two
-// launches (4.6, 7.1 and 4.6 with the counts in a launch of their own). Copies are bound by bytes.
+// 4096 pages. 8 rows that are emptied and grown again by up to 2048 tokens each, in a book of 8192 pages: 11.9 us, 2.7
+// emptying, 4.8 taking, 4.8 the slots. 64 rows emptied and forked from 16: 2.8, 6.1 taking, 2.9 sharing. Sums over lanes go
+// by DPP (through LDS, in 64 bits, the 8 rows took 15.3 us for 12.7), the slots of many tokens are a launch of their own
+// (in the one workgroup 17.8), and a free page's row is looked for by a thread for each page in order, behind barriers that
+// wait for LDS alone (by the thread that read the page's count, four one after the other, taking took 5.6 and 8.0 us). The
+// moves of 4096 pages: 4.7 and 4.6 in two launches (4.6, 7.1 and 4.6 with the counts in a launch of their own). Copies are
+// bound by bytes.
 
 #include <string.h>
 
@@ -36,6 +39,14 @@ __device__ __forceinline__ uint32_t wave_sums(uint32_t x) {  // inclusive
   return add_from<0x143, 0xc>(x);  // the end of row 1 into rows 2 and 3
 }
 
+// Barrier for what is in LDS: loads and stores of global memory stay under way across it.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // Two 32-bit numbers that are summed side by side.
 struct Pair {
   uint32_t a, b;
@@ -54,7 +65,7 @@ __device__ __forceinline__ Pair group_sums(Pair x, Pair (&room)[WAVES], Pair& al
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = static_cast<int>(threadIdx.x) & 63;
   const Pair s = {wave_sums(x.a), wave_sums(x.b)};
   if (lane == 63) room[wave] = s;
-  __syncthreads();
+  lds_barrier();
   const Pair w = lane < WAVES ? room[lane] : Pair{0, 0};
   const Pair upto = {wave_sums(w.a), wave_sums(w.b)};  // those up to each wavefront
   const auto at = [&](int l) {
@@ -146,6 +157,7 @@ __global__ __launch_bounds__(kMost) void qkn_pages_take(const TakeParams p) {
   __shared__ Pair room[2][kTakeWaves];
   __shared__ __align__(16) int32_t rows[kMost];
   __shared__ int32_t upto[kMost], first[kMost], tokens[kMost], length[kMost];
+  __shared__ int32_t got[4 * kMost];  // free pages in order
   const int i = static_cast<int>(threadIdx.x), shift = p.b.page_shift;
   const int64_t most = p.b.ld_table << shift;
   // the first pages' counts are asked for before they are needed
@@ -162,11 +174,9 @@ __global__ __launch_bounds__(kMost) void qkn_pages_take(const TakeParams p) {
   int64_t more = i < p.n && !FORK ? p.count[i] : 0;
   rows[i] = row;
   bool fine = row >= 0 && row < p.b.rows && from >= 0 && from < p.b.rows;
-  int64_t len = fine ? p.b.kv_len[from] : 0;
-  if (FORK && fine) fine = p.b.kv_len[row] == 0;
-  fine = fine && more >= 0 && len >= 0 && len + more <= most;
-  if (more < 0) more = 0;
-  __syncthreads();
+  const int64_t len = fine ? p.b.kv_len[from] : 0;
+  const int32_t old = FORK && fine ? p.b.kv_len[row] : 0;
+  lds_barrier();
   if (p.which) {  // listed before
     for (int j = 0; j < i && fine; j += 4) {
       const i32x4 r = *reinterpret_cast<const i32x4*>(&rows[j]);
@@ -174,8 +184,12 @@ __global__ __launch_bounds__(kMost) void qkn_pages_take(const TakeParams p) {
       for (int e = 0; e < 4; ++e) fine = fine && !(j + e < i && r[e] == row);
     }
   }
+  fine = fine && old == 0 && more >= 0 && len >= 0 && len + more <= most;
+  if (more < 0) more = 0;
   const int64_t have = FORK ? len >> shift : pages_for(len, shift);
   const int64_t need = fine ? pages_for(len + more, shift) - have : 0;
+  // no call's row is both: `from` has tokens here, and `to` none
+  const int32_t last = FORK && need ? p.b.table[from * p.b.ld_table + have] : -1;
   Pair all_needs, all_more = {0, 0};
   const int64_t ends = together(group_sums<kTakeWaves>(apart(need), room[0], all_needs)), total = together(all_needs);
   const int64_t token_end = FORK ? 0 : together(group_sums<kTakeWaves>(apart(more), room[1], all_more));
@@ -184,7 +198,7 @@ __global__ __launch_bounds__(kMost) void qkn_pages_take(const TakeParams p) {
   first[i] = static_cast<int32_t>(have);
   length[i] = static_cast<int32_t>(len);
   if (!FORK) tokens[i] = cut(token_end);
-  __syncthreads();
+  lds_barrier();
 
   // free pages, lowest first, to the needs in order
   int64_t found = 0;
@@ -199,27 +213,27 @@ __global__ __launch_bounds__(kMost) void qkn_pages_take(const TakeParams p) {
     int64_t start = found;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int half = 16 * (k % 2);
-      int64_t rank = start + (((k < 2 ? before.a : before.b) >> half) & 0xffff);
+      const int half = 16 * (k % 2), here = ((k < 2 ? all.a : all.b) >> half) & 0xffff;
+      if (here == 0 || start >= total) continue;
+      int at = ((k < 2 ? before.a : before.b) >> half) & 0xffff;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (r[k][e] != 0) continue;
-        if (rank < total) {
-          const int32_t page = static_cast<int32_t>(base + (k * kMost + i) * 4 + e);
-          const int at = holder(upto, p.n, static_cast<int32_t>(rank));
-          const int64_t entry = first[at] + (rank - (at ? upto[at - 1] : 0));
-          p.b.table[rows[at] * p.b.ld_table + entry] = page;
-          p.b.refs[page] = 1;
-          if (FORK) p.dst[at] = page;
-        }
-        ++rank;
+      for (int e = 0; e < 4; ++e)
+        if (r[k][e] == 0) got[at++] = static_cast<int32_t>(base + (k * kMost + i) * 4 + e);
+      lds_barrier();
+      for (int x = i; x < here && start + x < total; x += kMost) {
+        const int32_t page = got[x], rank = static_cast<int32_t>(start + x);
+        const int to = holder(upto, p.n, rank);
+        p.b.table[rows[to] * p.b.ld_table + first[to] + (rank - (to ? upto[to - 1] : 0))] = page;
+        p.b.refs[page] = 1;
+        if (FORK) p.dst[to] = page;
       }
-      start += ((k < 2 ? all.a : all.b) >> half) & 0xffff;
+      lds_barrier();
+      start += here;
     }
     found = start;
-    __syncthreads();  // room
+    lds_barrier();  // room
   }
-  __syncthreads();  // the table's entries are there
+  if (!FORK || found < total) __syncthreads();  // the table's entries are there
 
   const bool served = fine && (need == 0 || ends <= found);
   if (need > 0 && !served) {  // gives back what it got, if it is the first that did not get all
@@ -229,14 +243,14 @@ __global__ __launch_bounds__(kMost) void qkn_pages_take(const TakeParams p) {
     p.done[i] = served ? static_cast<int32_t>(len + more) : -1;
     if (served) p.b.kv_len[row] = static_cast<int32_t>(len + more);
     if (FORK) {
-      p.src[i] = served && need ? p.b.table[from * p.b.ld_table + have] : -1;
+      p.src[i] = served && need ? last : -1;
       if (!(served && need)) p.dst[i] = -1;
     }
   }
   if constexpr (!FORK) {
     if ((!p.slots && !p.pos) || p.T > 4 * kMost) return;  // qkn_pages_slots
     if (!served) first[i] = -1;
-    __syncthreads();
+    lds_barrier();
     list_tokens<kMost>(p, rows, length, first, tokens, all_tokens, i);
   }
 }
@@ -267,7 +281,7 @@ __global__ __launch_bounds__(kManyThreads) void qkn_pages_slots(const TakeParams
     end += count[e];
     tokens[i0 + e] = static_cast<int32_t>(end < 0x7fffffff ? end : 0x7fffffff);
   }
-  __syncthreads();
+  lds_barrier();
   list_tokens<kManyThreads>(p, rows, length, first, tokens, all, static_cast<int64_t>(blockIdx.x) * kMany + threadIdx.x);
 }
 

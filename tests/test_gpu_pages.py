@@ -203,6 +203,33 @@ def test_large_books(pages):
     assert got.held() == [[where.get(p, p) for p in row] for row in b.ref.held()]
 
 
+@pytest.mark.parametrize("pages,every", [(5000, 1), (40000, 3), (70001, 7)])
+def test_many_pages_at_once(pages, every):
+    """More pages than one pass over the book finds, some passes with few or none; a row that does not get all of them."""
+    b = Both(pages, 40, 1 << 14, 2)
+    refs = np.ones(pages, np.int32)
+    refs[::every] = 0
+    refs[4096:8192] = 1  # a part without free pages
+    refs[20000:37000] = 1
+    b.dev.refs.copy_(torch.from_numpy(refs))
+    b.ref.refs[:] = refs
+    free = int((refs == 0).sum())
+    counts = [2 * (free // 5) - 1, 0, 1, 2 * (free // 2), 3, 2 * free, 0, 1]
+    counts = [min(c, 1 << 14) for c in counts]
+    done = qkn.qkn_pages_grow(b.dev, _i32(counts))
+    want = b.ref.grow(counts, None, 0)
+    assert _ints(done) == [int(x) for x in want[0]]
+    got = O.Book(*(t.cpu().numpy() for t in (b.dev.refs, b.dev.table, b.dev.kv_len)), 2)
+    assert np.array_equal(got.refs, b.ref.refs) and np.array_equal(got.kv_len, b.ref.kv_len) and got.held() == b.ref.held()
+    rows = list(range(8, 40))
+    call = qkn.PreparedPagesFork(b.dev, _i32([0, 2] * 16), _i32(rows), _i32([77] * 32), _i32([77] * 32), _i32([77] * 32))
+    call()
+    want = b.ref.fork([0, 2] * 16, rows)
+    assert [_ints(call.done), _ints(call.src), _ints(call.dst)] == [list(map(int, w)) for w in want]
+    got = O.Book(*(t.cpu().numpy() for t in (b.dev.refs, b.dev.table, b.dev.kv_len)), 2)
+    assert np.array_equal(got.refs, b.ref.refs) and np.array_equal(got.kv_len, b.ref.kv_len) and got.held() == b.ref.held()
+
+
 def test_malformed_books_stay_inside_their_arrays():
     """Lengths and page numbers outside their ranges; what lies around the arrays keeps its values."""
     room = {n: torch.full((k + 64,), 1234, dtype=torch.int32, device=DEV) for n, k in (("refs", 8), ("table", 20), ("kv_len", 5))}
