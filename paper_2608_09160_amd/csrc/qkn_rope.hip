@@ -16,15 +16,15 @@
 // A 4-bit cache's blocks are four lanes' groups (where pairs are apart) or two lanes' both groups: the largest magnitude
 // crosses lanes by DPP, as integers, and the exponent is a carry from the mantissa. Rows that no vector fits, and heads that
 // do not put a block on neighbouring lanes, take half a wavefront for a block of 32. 8192 tokens of 16 + 4 + 4 heads, 88 MB,
-// 23.0 us, half of it the issue of vector instructions; two tokens a wavefront, which share gamma, were slower (25.4 for
-// 24.4 at that time).
+// 23.0 us: 247 vector instructions a wavefront, issued for 10 of them; two tokens a wavefront, which share gamma, were
+// slower (25.4 for 24.4 at that time).
 // Instructions count beside the bytes, so what would only move registers is not there: a kernel for each layout of pairs,
-// rows and slots addressed for all lanes at once, and lanes without gamma multiplied by 1 (16 + 4 + 4 heads over 4 bits, 351
-// vector instructions for 562 in the code, 24.4 -> 23.0 us; the cases below 24.5 -> 23.2, 70.7 -> 70.2, 5.4 -> 4.5).
+// rows and slots addressed for all lanes at once, and lanes without gamma multiplied by 1 (16 + 4 + 4 heads over 4 bits, 354 ->
+// 247 vector instructions a wavefront, 24.4 -> 23.0 us; the cases below 24.5 -> 23.2, 70.7 -> 70.2, 5.4 -> 4.5).
 // Measured: 8192 tokens of 16 + 4 + 4 heads of 128 with the norm, bf16 cache, 105 MB: 23.2 us, 4.5 TB/s; 32768 tokens of
 // 16 + 2 + 2 heads into an FP8 cache, 337 MB: 70 us, 4.8 TB/s; a copy of as many bytes reaches 5 to 5.9. 64 tokens: 4.5 us, a
 // launch and one chain of latencies (position -> angles). Element by element (V = 1) 8192 tokens of 16 + 4 + 4 heads of 50,
-// 41 MB, take 37.5 us; of 48, in vectors, 12.8.
+// 41 MB, take 34.7 us; of 48, in vectors, 11.8.
 
 #include <string.h>
 
