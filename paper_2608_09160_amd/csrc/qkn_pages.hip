@@ -158,6 +158,7 @@ __global__ __launch_bounds__(kMost) void qkn_pages_take(const TakeParams p) {
   __shared__ __align__(16) int32_t rows[kMost];
   __shared__ int32_t upto[kMost], first[kMost], tokens[kMost], length[kMost];
   __shared__ int32_t got[4 * kMost];  // free pages in order
+  __shared__ struct { int64_t entry; int32_t count; } partly;  // the table's entries of a row that did not get all its pages
   const int i = static_cast<int>(threadIdx.x), shift = p.b.page_shift;
   const int64_t most = p.b.ld_table << shift;
   // the first pages' counts are asked for before they are needed
@@ -173,6 +174,7 @@ __global__ __launch_bounds__(kMost) void qkn_pages_take(const TakeParams p) {
   const int32_t from = i < p.n && FORK ? p.from[i] : row;
   int64_t more = i < p.n && !FORK ? p.count[i] : 0;
   rows[i] = row;
+  if (i == 0) partly = {0, 0};
   bool fine = row >= 0 && row < p.b.rows && from >= 0 && from < p.b.rows;
   const int64_t len = fine ? p.b.kv_len[from] : 0;
   const int32_t old = FORK && fine ? p.b.kv_len[row] : 0;
@@ -236,8 +238,24 @@ __global__ __launch_bounds__(kMost) void qkn_pages_take(const TakeParams p) {
   if (!FORK || found < total) __syncthreads();  // the table's entries are there
 
   const bool served = fine && (need == 0 || ends <= found);
-  if (need > 0 && !served) {  // gives back what it got, if it is the first that did not get all
-    for (int64_t x = 0; x < need && ends - need + x < found; ++x) p.b.refs[p.b.table[row * p.b.ld_table + have + x]] = 0;
+  if (found < total) {
+    // The first row that did not get all of its pages gives back what it got: all threads do, four entries each at a time.
+    // A row refused in a pool of 65536 pages takes 39.6 us, a served one 34.3 (by that row's thread, each entry behind the one
+    // before, 7.4 ms).
+    if (need > 0 && !served && ends - need < found) {
+      partly.entry = row * p.b.ld_table + have;
+      partly.count = static_cast<int32_t>(found - (ends - need));
+    }
+    lds_barrier();
+    const int32_t* entries = p.b.table + partly.entry;
+    for (int32_t x0 = i; x0 < partly.count; x0 += 4 * kMost) {
+      int32_t page[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) page[k] = x0 + k * kMost < partly.count ? entries[x0 + k * kMost] : -1;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (page[k] >= 0) p.b.refs[page[k]] = 0;
+    }
   }
   if (i < p.n) {
     p.done[i] = served ? static_cast<int32_t>(len + more) : -1;

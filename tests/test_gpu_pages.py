@@ -391,3 +391,45 @@ def test_calls_on_a_given_stream():
     want = b.ref.compact(30)
     b.same()
     assert [_ints(src), _ints(dst)] == [list(map(int, w)) for w in want]
+
+
+@pytest.mark.parametrize("free", [3, 1023, 1026, 4099, 20011])
+def test_what_a_refused_row_got_is_free_again(free):
+    b = Both(free + 7, 4, free + 100, 1)
+    b.grow([3, 0, 4, 0])
+    b.grow([2, free, 1, 0])  # the second row is two pages short, and nothing is left for the third
+    assert b.ref.kv_len.tolist() == [5, 0, 4, 0]
+    b.grow([0, free - 2, 0, 0])  # all of them are there
+    b.grow([1, 1, 0, 1])
+
+
+def _least_us(call, before):
+    spent = []
+    for _ in range(4):
+        before()
+        torch.cuda.synchronize()
+        begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        begin.record()
+        call()
+        end.record()
+        torch.cuda.synchronize()
+        spent.append(1e3 * begin.elapsed_time(end))
+    return min(spent)
+
+
+def test_a_refused_row_takes_no_longer_than_a_served_one():
+    """A captured loop meets an empty pool on every replay: giving pages back is as wide as handing them out. Both read the
+    pool once and write an entry a page; a thread that gave 65536 pages back by itself took 200 times the served call."""
+    pages = 65536
+    book = qkn.PageBook.empty(pages, 2, pages + 1, 1, DEV)
+    served, refused = (qkn.PreparedPagesGrow(book, _i32([n, 0])) for n in (pages, pages + 1))
+
+    def empty():
+        book.refs.zero_()
+        book.kv_len.zero_()
+
+    there = _least_us(served, empty)
+    assert _ints(served.done) == [pages, 0] and int(book.refs.sum()) == pages
+    gone = _least_us(refused, empty)
+    assert _ints(refused.done) == [-1, 0] and int(book.refs.sum()) == 0
+    assert gone < 8 * there, (gone, there)
