@@ -20,6 +20,9 @@ __attribute__((visibility("hidden"))) int set_proj_tile(int64_t choice);
 // Records the calling thread's latest launch for qkn_last_launch.
 __attribute__((visibility("hidden"))) void record_launch(const qkn_launch_info& info);
 
+// Whether HIP takes a launch of so many workgroups in a dimension of the grid: it counts the threads in 32 bits.
+inline bool launchable(int64_t blocks, int64_t threads) { return blocks * threads < int64_t{1} << 32; }
+
 // A strided byte region: `rows` rows of `width` elements every `ld` elements.
 struct Span {
   uintptr_t base;

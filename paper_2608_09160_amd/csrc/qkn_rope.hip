@@ -520,13 +520,17 @@ int rope_impl(const qkn_rope_seg* q, const qkn_rope_seg* k, const uint16_t* v, i
   // K and V of a 4-bit cache that do not fit the vectors go by themselves, before K's rows may be written in place
   const bool elements = cache4 && !(vec && fit4);
   const int64_t blocks = elements ? ((k ? n_kv : 0) + (v ? n_kv : 0)) * (D / 32) : 0;
+  if (T >= int64_t{1} << 31) return QKN_ENOTSUP;
+  const int64_t grid4 = (T * blocks + 2 * kWaves - 1) / (2 * kWaves);
   if (elements) {
-    if (T * blocks > (int64_t{1} << 31) - 8) return QKN_ENOTSUP;
     units[2] = 0;
     if (k && !k->y) units[1] = 0;
   }
   const int64_t all = units[0] + units[1] + units[2], parts = all ? (all + 63) / 64 : 1;
-  if (all > most || T > (int64_t{1} << 31) - 8 || T * parts > (int64_t{1} << 31) - 8) return QKN_ENOTSUP;
+  const int64_t grid = (T * parts + kWaves - 1) / kWaves;
+  // both launches, before either writes
+  if (all > most || !qkn_host::launchable(grid4, 64 * kWaves) || (all && !qkn_host::launchable(grid, 64 * kWaves)))
+    return QKN_ENOTSUP;
 
   RopeParams p;
   memset(&p, 0, sizeof(p));
@@ -577,7 +581,6 @@ int rope_impl(const qkn_rope_seg* q, const qkn_rope_seg* k, const uint16_t* v, i
   }
 
   const Format f = cache4 ? kFp4 : cache && cache->fp8 ? kFp8 : kBf16;
-  const int64_t grid = (T * parts + kWaves - 1) / kWaves;
   const char* name = elements ? "rope4/elements" : f == kFp4 ? "rope<8>/fp4"
                      : vec    ? (f == kFp8 ? "rope<8>/fp8" : "rope<8>/bf16")
                               : (f == kFp8 ? "rope<1>/fp8" : "rope<1>/bf16");
@@ -590,9 +593,8 @@ int rope_impl(const qkn_rope_seg* q, const qkn_rope_seg* k, const uint16_t* v, i
     Elements4 x{fast_div(static_cast<uint32_t>(blocks)), fast_div(static_cast<uint32_t>(D / 32)),
                 static_cast<int32_t>(k ? n_kv * (D / 32) : 0)};
     void* args[] = {&p, &x};
-    if (hipLaunchKernel(reinterpret_cast<const void*>(qkn_rope4_elements),
-                        dim3(static_cast<unsigned>((T * blocks + 2 * kWaves - 1) / (2 * kWaves))), dim3(64 * kWaves), args, 0,
-                        st) != hipSuccess)
+    if (hipLaunchKernel(reinterpret_cast<const void*>(qkn_rope4_elements), dim3(static_cast<unsigned>(grid4)),
+                        dim3(64 * kWaves), args, 0, st) != hipSuccess)
       return QKN_EHIP;
     p.cached = 0;  // the rest writes rows only
   }

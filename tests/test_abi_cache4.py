@@ -199,6 +199,26 @@ def test_write_paths(dry, kw, kernel):
     assert L.qkn_last_launch()["kernel"] == kernel
 
 
+def test_writes_of_2_32_threads_are_refused(dry):
+    """As QKN_ENOTSUP before anything is written: half a wavefront takes 32 elements, and a wavefront a token's rows."""
+    far = dict(q=None, v=None, ldv=0, table=1 << 50, pos=1 << 51, slots=1 << 52, tp=1, rot=32)
+    k = dict(x=1 << 40, w=None, partials=None, d_full=0)
+    for T, want in (((1 << 24) - 1, DRY), (1 << 24, L.QKN_ENOTSUP)):  # 8 blocks a token, 8 to a workgroup
+        assert rope4(dry, T=T, k=seg(300, 2, y=None, **k), **far) == want
+        if want == DRY:
+            assert L.qkn_last_launch()["kernel"] == "rope4/elements"
+    # one block a token, and rows besides: the second launch's limit, found before the first
+    k.update(x=1 << 40, ldx=32)
+    c = cache(32, n_kv=1)
+    far.update(D=32, cache=c)
+    most = 4 * ((1 << 24) - 1)
+    for T, want in ((most, DRY), (most + 1, L.QKN_ENOTSUP)):
+        assert rope4(dry, T=T, k=seg(300, 1, 32, y=1 << 45, **k), **far) == want
+    # rows that are not written need no second launch
+    for T, want in ((2 * most, DRY), (2 * most + 8, L.QKN_ENOTSUP)):
+        assert rope4(dry, T=T, k=seg(300, 1, 32, y=None, **k), **far) == want
+
+
 def test_reading_back(dry):
     assert load4(dry, k=None, v=None) == L.QKN_EINVAL
     assert load4(dry, slots=None) == L.QKN_EINVAL and load4(dry, T=-1) == L.QKN_EINVAL

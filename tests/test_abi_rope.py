@@ -97,6 +97,14 @@ def test_size_limits(dry):
                 pos=1 << 51) == L.QKN_ENOTSUP
 
 
+def test_launches_of_2_32_threads_are_refused(dry):
+    """As QKN_ENOTSUP by the validation, not as QKN_EHIP by the launch: four wavefronts a workgroup, one a token."""
+    most = 4 * ((1 << 24) - 1)
+    for T, want in ((most, DRY), (most + 1, L.QKN_ENOTSUP)):
+        q = seg(0, 8, w=None, partials=None, d_full=0, x=1 << 40, y=1 << 42)
+        assert call(dry, T=T, q=q, k=None, v=None, cache=None, table=1 << 50, pos=1 << 51) == want
+
+
 @pytest.mark.parametrize("kw", [
     dict(q=seg(0, 8, y=BASE + 2)),                     # y one element into x
     dict(q=seg(0, 8, y=BASE + 300 * MB)),              # Q's output on K's input
