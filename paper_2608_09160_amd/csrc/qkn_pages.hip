@@ -769,7 +769,7 @@ int qkn_pages_compact(const qkn_pages* book, const qkn_pages* out, int32_t* src,
   if (!aligned(workspace, 16)) return QKN_ENOTSUP;
   int64_t work = (book->num_pages + entries + kRowThreads - 1) / kRowThreads;
   if (work == 0) work = 1;  // the lists alone
-  if (work >= int64_t{1} << 31) return QKN_ENOTSUP;
+  if (!qkn_host::launchable(work, kRowThreads)) return QKN_ENOTSUP;  // before the list of moves is written
   Arrays a;
   a.book(*book);
   if (out->refs != book->refs) a.add(out->refs, out->num_pages, 4, true);

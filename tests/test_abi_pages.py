@@ -83,6 +83,14 @@ def test_refusals(dry):
     assert calls(dry, book(), ws=BASE + 150 * MB + 4)[3] == L.QKN_ENOTSUP
 
 
+def test_moves_of_2_32_threads_are_refused(dry):
+    """As QKN_ENOTSUP, before a list of moves is written that no launch then carries out: a thread a page and a table entry."""
+    far = dict(refs=1 << 40, table=1 << 41, kv_len=1 << 50, num_pages=256, page_size=1, rows=(1 << 16) - 1)
+    for ld, want in ((1 << 16, DRY), ((1 << 16) + 1, L.QKN_ENOTSUP), (1 << 30, L.QKN_ENOTSUP)):
+        assert (256 + ld * far["rows"] < 1 << 32) == (want == DRY)
+        assert calls(dry, book(ld_table=ld, **far))[3] == want
+
+
 def test_overlap(dry):
     o = L.QKN_EOVERLAP
     for at in (0, 10, 20):  # the book's arrays
