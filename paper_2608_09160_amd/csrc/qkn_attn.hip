@@ -256,7 +256,10 @@ int attn_impl(const qkn_attn_args* args, int32_t sinks, const Source* cache, voi
       (pl.ws_bytes && !aligned(workspace, 16)))
     return QKN_ENOTSUP;
   const int64_t rows = a.T * a.n_q;
-  if (pl.grid >= int64_t{1} << 31) return QKN_ENOTSUP;
+  const bool join_few = rows <= kJoinFew;
+  const int64_t join_grid = join_few ? rows : (rows + 7) / 8;
+  if (!qkn_host::launchable(pl.grid, pl.v.threads) || (pl.split && !qkn_host::launchable(join_grid, kJoinThreads)))
+    return QKN_ENOTSUP;
 
   const int64_t width = int64_t{a.n_q} * c.head_dim;
   const Span in[] = {Span{reinterpret_cast<uintptr_t>(a.q), a.T, a.ldq, width, 2},
@@ -321,10 +324,8 @@ int attn_impl(const qkn_attn_args* args, int32_t sinks, const Source* cache, voi
   if (pl.split) {
     int32_t tile_rows = pl.v.rows;
     void* jargs[] = {&p, &tile_rows};
-    const bool few = rows <= kJoinFew;
-    const dim3 jgrid(static_cast<unsigned>(few ? rows : (rows + 7) / 8),
-                     static_cast<unsigned>((c.head_dim + 4 * kJoinVecs - 1) / (4 * kJoinVecs)));
-    const void* join = few ? reinterpret_cast<const void*>(qkn_attn_join<8>) : reinterpret_cast<const void*>(qkn_attn_join<1>);
+    const dim3 jgrid(static_cast<unsigned>(join_grid), static_cast<unsigned>((c.head_dim + 4 * kJoinVecs - 1) / (4 * kJoinVecs)));
+    const void* join = join_few ? reinterpret_cast<const void*>(qkn_attn_join<8>) : reinterpret_cast<const void*>(qkn_attn_join<1>);
     if (hipLaunchKernel(join, jgrid, dim3(kJoinThreads), jargs, 0, st) != hipSuccess)
       return QKN_EHIP;
   }

@@ -134,6 +134,21 @@ def test_workspace(dry):
     assert dry.qkn_attn4_workspace_bytes(ctypes.byref(a), None) == L.QKN_EINVAL
 
 
+def test_attention_of_2_32_threads_is_refused(dry):
+    """As QKN_ENOTSUP by the validation, not as QKN_EHIP by a launch: 16 rows to a workgroup of 256 threads, a workgroup more for
+    the sequence, 8 heads of keys; and the joining of split keys, 8 rows to one."""
+    c = dict(n_kv=8, k_page=8 * 512, v_page=8 * 512, ke_page=8 * 32, ve_page=8 * 32)
+    far = dict(q=1 << 40, ldq=512, out=1 << 41, ldo=512, lse=None, n_q=8, max_q=1)
+    most = 16 * ((1 << 21) - 2) + 15
+    for T, want in ((most, DRY), (most + 1, L.QKN_ENOTSUP)):
+        assert attn4(dry, args(T=T, batch=1, max_kv=16, **far), cache(64, **c)) == want  # few keys: not split
+    most = (1 << 24) - 1  # 8 rows a token
+    for T, want in ((most, DRY), (most + 1, L.QKN_ENOTSUP)):
+        a = args(T=T, batch=1, max_kv=1 << 16, ld_table=1 << 12, **far)
+        need = dry.qkn_attn4_workspace_bytes(ctypes.byref(a), ctypes.byref(cache(64, **c)))
+        assert need > 0 and attn4(dry, a, cache(64, **c), ws_bytes=need) == want
+
+
 MALFORMED = [dict(num_pages=-1), dict(page_size=24), dict(page_size=0), dict(n_kv=0), dict(head_dim=0), dict(head_dim=48),
              dict(k_token=63), dict(v_head=0), dict(ke_token=3), dict(ve_page=-4), dict(k_page=(1 << 40) + 1)]
 
