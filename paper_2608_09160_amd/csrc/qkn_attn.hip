@@ -93,7 +93,9 @@ constexpr int kMinPart = 4;
 // whole and split: 32 over up to 16384 keys, 32 + 8 heads 133 and 72.6, 48 162 and 98.9, over 16384 each 175 and 162; 64
 // over up to 4096, 16 + 8 heads 47.4 and 43.0; 32 of 4 tokens over up to 8192, 64 + 8 heads 76.3 and 51.8). Equal lengths
 // can lose (64 over 8192 each, 16 + 8 heads 104 and 110; heads of 256, 32 over 4096 each, 64 + 8 heads 60.9 and 65.0), and
-// so do short ones (64 over 2048 each, 8 + 8 heads 31.6 and 36.1).
+// so do short ones (64 over 2048 each, 8 + 8 heads 31.6 and 36.1). First tokens beside a window are among the keys (over up to
+// 16384, 32 + 8 heads: 32 with a window of 1024 and 6000 first tokens 58.6 and 47.8, of 256 and 12000 104 and 63.6; 64 of 16 + 8
+// heads 91.3 and 93.7, 140 and 139).
 constexpr int64_t kLongParts = 8;
 // Pairs of 64 rows and 64 keys up to which many-row launches take 64 rows to a workgroup (16 + 4 heads of 128, us with 64
 // and with 128 rows: prompts of 256 tokens 9.6 and 12.2, 1024 21.7 and 26.6, 2048 39.1 and 49.7, 8192 344 and 277; 128
@@ -173,7 +175,7 @@ int check_sizes(const qkn_attn_args* a, int32_t sinks, const Source* c) {
 }
 
 // The workgroups of kernel v, and their workspace.
-Plan plan_with(const qkn_attn_args& a, const Source& c, const Variant& v) {
+Plan plan_with(const qkn_attn_args& a, int32_t sinks, const Source& c, const Variant& v) {
   Plan pl{};
   pl.v = v;
   const int64_t group = a.n_q / c.n_kv;
@@ -190,7 +192,9 @@ Plan plan_with(const qkn_attn_args& a, const Source& c, const Variant& v) {
     const int64_t most = pl.items * ((a.max_kv + part - 1) / part);
     pl.items = slots < most ? slots : most;
   } else if (c.format == kFp4 && a.batch) {
-    const int64_t full = int64_t{pl.v.fit} * kCus / c.n_kv, keys = a.window && a.window < a.max_kv ? a.window : a.max_kv;
+    const int64_t full = int64_t{pl.v.fit} * kCus / c.n_kv;
+    int64_t keys = a.max_kv;
+    if (a.window && int64_t{a.window} + sinks < keys) keys = int64_t{a.window} + sinks;
     // row tiles of max_q tokens a sequence; sequences may have more, which the workgroups have to suffice for
     const int64_t each = ((a.max_q < 1 ? 1 : a.max_q) * group + pl.v.rows - 1) / pl.v.rows * a.batch;
     pl.split = 2 * (each < pl.items ? each : pl.items) <= full && keys >= kLongParts * part;
@@ -224,8 +228,8 @@ Plan plan_of(const qkn_attn_args& a, int32_t sinks, const Source& c, int64_t* wo
   whole.window = 0;
   if (few) {
     const Variant v = few_rows_of(c, sinks, dt, static_cast<int>(rows));
-    if (workspace_bytes) *workspace_bytes = plan_with(whole, c, v).ws_bytes;
-    return plan_with(a, c, v);
+    if (workspace_bytes) *workspace_bytes = plan_with(whole, 0, c, v).ws_bytes;
+    return plan_with(a, sinks, c, v);
   }
   // keys that a row sees, about, and pairs of 64 rows and 64 keys in all
   int64_t keys = a.max_kv - (a.causal ? (a.max_q < a.max_kv ? a.max_q : a.max_kv) / 2 : 0);
@@ -233,10 +237,10 @@ Plan plan_of(const qkn_attn_args& a, int32_t sinks, const Source& c, int64_t* wo
   const int64_t pairs = (a.T * group + 63) / 64 * c.n_kv * ((keys + 63) / 64);
   const Variant small = many_rows_of(c, sinks, dt, true), large = many_rows_of(c, sinks, dt, false);
   if (workspace_bytes) {
-    const int64_t s = plan_with(whole, c, small).ws_bytes, l = plan_with(whole, c, large).ws_bytes;
+    const int64_t s = plan_with(whole, 0, c, small).ws_bytes, l = plan_with(whole, 0, c, large).ws_bytes;
     *workspace_bytes = s > l ? s : l;
   }
-  return plan_with(a, c, pairs <= kSmallPairs ? small : large);
+  return plan_with(a, sinks, c, pairs <= kSmallPairs ? small : large);
 }
 
 int attn_impl(const qkn_attn_args* args, int32_t sinks, const Source* cache, void* workspace, int64_t workspace_bytes,

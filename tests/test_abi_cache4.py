@@ -134,6 +134,22 @@ def test_workspace(dry):
     assert dry.qkn_attn4_workspace_bytes(ctypes.byref(a), None) == L.QKN_EINVAL
 
 
+@pytest.mark.parametrize("T,batch,max_q,n_kv,keys", [(64, 64, 1, 8, 4096), (40, 40, 1, 8, 4096), (1500, 20, 64, 4, 2048)])
+def test_first_tokens_count_where_long_keys_are_split(dry, T, batch, max_q, n_kv, keys):
+    """A row reads its first tokens besides its window: with that many together the keys are split (into a workspace) where
+    a window of as many would be."""
+    c = cache(n_kv=n_kv, num_pages=8, k_page=16 * 64 * n_kv, v_page=16 * 64 * n_kv, ke_page=64 * n_kv, ve_page=64 * n_kv)
+    for window, sinks, split in ((keys, 0, True), (keys - 1, 0, False), (64, keys - 64, True), (64, keys - 65, False),
+                                 (1, 2 ** 31 - 1, True), (2 ** 31 - 1, 2 ** 31 - 1, True)):
+        a = args(T=T, batch=batch, max_q=max_q, max_kv=16384, ld_table=1024, window=window)
+        assert attn4(dry, a, c, sinks, ws=None, ws_bytes=0) == (L.QKN_EINVAL if split else DRY), (window, sinks)
+        need = dry.qkn_attn4_workspace_bytes(ctypes.byref(a), ctypes.byref(c))
+        assert attn4(dry, a, c, sinks, ws_bytes=need) == DRY
+        # as many keys as the sequences have at most
+        a = args(T=T, batch=batch, max_q=max_q, max_kv=keys - 1, ld_table=1024, window=window)
+        assert attn4(dry, a, c, sinks, ws=None, ws_bytes=0) == DRY
+
+
 def test_attention_of_2_32_threads_is_refused(dry):
     """As QKN_ENOTSUP by the validation, not as QKN_EHIP by a launch: 16 rows to a workgroup of 256 threads, a workgroup more for
     the sequence, 8 heads of keys; and the joining of split keys, 8 rows to one."""

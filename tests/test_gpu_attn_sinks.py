@@ -175,6 +175,17 @@ def test_many_sequences_of_unequal_lengths(hq, hk, D, most, window, sinks):
         batch.check(*batch.run(window=window, sinks=sinks, max_q=max_q), window=window, sinks=sinks, heads=[0, hq - 1])
 
 
+@pytest.mark.parametrize("window,sinks", [(64, 4090), (1, 4500), (2000, 2100), (100, 100000)])
+@pytest.mark.parametrize("hq,hk,D", [(8, 8, 64), (16, 8, 128)])
+def test_many_sequences_with_many_first_tokens(hq, hk, D, window, sinks):
+    """As above: first tokens and a short window together are as many keys as are split."""
+    lens = [(1 + b % 3, (b * 37) % 150) for b in range(40)]
+    lens[0], lens[3], lens[17], lens[-1] = (3, 5000), (0, 0), (1, 4777), (2, 1024)
+    batch = Batch(hq + sinks, lens, hq, hk, D)
+    for max_q in (3, 1):
+        batch.check(*batch.run(window=window, sinks=sinks, max_q=max_q), window=window, sinks=sinks, heads=[0, hq - 1])
+
+
 @pytest.mark.parametrize("window,sinks", [(0, 0), (2500, 3), (50, 4)])
 def test_many_chunks_of_unequal_lengths(window, sinks):
     """As above, of more rows."""
