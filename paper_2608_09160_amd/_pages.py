@@ -135,12 +135,13 @@ class PreparedPagesFork(_Call):
 
 
 class PreparedPagesFree(_Call):
-    """qkn_pages_free: empties the rows `which` (int32)."""
+    """qkn_pages_free: empties the rows `which` (int32; None: every row of the book)."""
 
     _name = "qkn_pages_free"
 
-    def __init__(self, book: PageBook, which: torch.Tensor):
-        b, n = book.struct(), which.numel()
+    def __init__(self, book: PageBook, which: Optional[torch.Tensor] = None):
+        b = book.struct()
+        n = b.rows if which is None else which.numel()
         self.which = which
         self._prepare(book, ctypes.byref(b), _list(which, "which", n), n, keep=(b,))
 
@@ -206,7 +207,7 @@ def qkn_pages_fork(book, parents, to, caches=(), src=None, dst=None, stream=None
         return done
 
 
-def qkn_pages_free(book, which, stream=None) -> None:
+def qkn_pages_free(book, which=None, stream=None) -> None:
     """PreparedPagesFree made and called once."""
     with _on(stream):
         PreparedPagesFree(book, which)()

@@ -173,3 +173,11 @@ def test_bindings_checks():
         b.struct()  # not on a GPU
     with pytest.raises(TypeError):
         P.PreparedPagesCopy([S.KVCache(b.refs, b.refs), S.KVCache4(*[b.refs] * 4)], b.refs, b.refs)
+
+
+def test_freeing_without_a_list_is_of_every_row(dry, monkeypatch):
+    monkeypatch.setattr(P.PageBook, "struct", lambda self: book(rows=self.table.shape[0]))
+    for rows, want in ((0, L.QKN_OK), (1, DRY), (1024, DRY), (1025, L.QKN_ENOTSUP)):
+        free = P.PreparedPagesFree(P.PageBook.empty(4, rows, 16, 16, device="cpu"))
+        assert free._args[1:] == (None, rows)
+        assert free._fn(*free._args, None) == want

@@ -433,3 +433,20 @@ def test_a_refused_row_takes_no_longer_than_a_served_one():
     gone = _least_us(refused, empty)
     assert _ints(refused.done) == [-1, 0] and int(book.refs.sum()) == 0
     assert gone < 8 * there, (gone, there)
+
+
+def test_all_rows_are_freed_without_a_list():
+    b = Both(60, 6, 100, 16)
+    b.grow([40, 21, 5, 0, 100, 16])
+    b.fork([0], [3])
+    qkn.qkn_pages_free(b.dev)
+    b.ref.free(range(6))
+    b.same()
+    assert not b.ref.refs.any() and not b.ref.kv_len.any()
+    b.grow([100] * 6)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    qkn.PreparedPagesFree(b.dev)(side)
+    b.ref.free(range(6))
+    b.same()
+    qkn.qkn_pages_free(qkn.PageBook.empty(4, 0, 16, 16, DEV))
