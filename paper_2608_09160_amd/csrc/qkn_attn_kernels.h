@@ -60,8 +60,10 @@
 // Over 4 bits: 64 single tokens over up to 4096 keys, 37 MB, 16.8 us, and 16 over up to 32768, 84 MB, 23.6 us (the join 4.0 and
 // 4.4 of them): a wavefront's 12,600 turns of four cycles are 4,100 instructions issued (1,780 vector, 2,110 scalar) and half
 // waiting, for lengths, pages and the first tile one after the other in the first 4 us, then for the tiles. A prompt of 8192
-// tokens 309 us, 0.89 Pflop/s, bf16's cycles and a tenth for the widening; 128 single tokens over up to 8192 keys of 8 + 8
-// heads, not split, 134 us (bf16 414).
+// tokens 309 us, 0.89 Pflop/s: bf16's cycles and the widening, which every row tile does again. Over bf16 and over 4 bits, on
+// one card: prompts of 8192 tokens 298 and 343 us, of 2048 43.7 and 51.8, 777 tokens behind 11224 104.7 and 115.7, 4096 tokens of
+// heads of 256 202 and 225, 8192 of heads of 64 193 and 246. 128 single tokens over up to 8192 keys of 8 + 8 heads, not split,
+// 134 us (bf16 414).
 // Slower: the wavefronts in two groups that take turns at products and softmax (288 to 309 us), 64 rows a wavefront with
 // one tile's softmax between another's products (322), wave priorities by phase and operands fetched 1 to 10 products ahead
 // (within 4 %).

@@ -2,12 +2,16 @@
 //
 // The book's calls are integer work on small arrays, each a chain of latencies: taking pages is one workgroup, so that
 // ranks among the free pages and among the rows' needs need no second launch; the rest has a workgroup for a row or for
-// 4096 pages. 8 rows that are emptied and grown again by up to 2048 tokens each, in a book of 8192 pages: 11.9 us, 2.7
-// emptying, 4.8 taking, 4.8 the slots. 64 rows emptied and forked from 16: 2.8, 6.1 taking, 2.9 sharing. Sums over lanes go
-// by DPP (through LDS, in 64 bits, the 8 rows took 15.3 us for 12.7), the slots of many tokens are a launch of their own
-// (in the one workgroup 17.8), and a free page's row is looked for by a thread for each page in order, behind barriers that
-// wait for LDS alone (by the thread that read the page's count, four one after the other, taking took 5.6 and 8.0 us). The
-// moves of 4096 pages: 4.7 and 4.6 in two launches (4.6, 7.1 and 4.6 with the counts in a launch of their own). Copies are
+// 4096 pages. 8 rows that are emptied and grown again by up to 2048 tokens each, in a book of 8192 pages: 11.7 us; 64 rows
+// emptied and forked from 16, with the copies of four layers: 18.9. (Of a profiler's dispatches, which are longer than the
+// same launches in a row without it: 2.7 emptying, 4.7 taking, 4.9 the slots; 2.6, 5.9 taking, 2.6 sharing, 8.1 the copy.)
+// Sums over lanes go by DPP (through LDS, in 64 bits, the 8 rows took 15.3 us for 12.7), the slots of many tokens are a launch
+// of their own (in the one workgroup 17.8), and a free page's row is looked for by a thread for each page in order, behind
+// barriers that wait for LDS alone (by the thread that read the page's count, four one after the other, taking took 5.6 and
+// 8.0 us in the profiler). Free pages are looked for 16384 pages a pass, each pass a trip to memory behind the one before,
+// and lowest-first packs the pages in use at the front: 64 rows that need a page each behind 7360 used pages of 8192 take 5.1
+// us, behind 58944 of 65536 8.6, behind 471808 of 524288 38.9; rows that need none 3.0 whatever the pool. The moves of 4096
+// pages: 4.7 and 4.6 in two launches (4.6, 7.1 and 4.6 with the counts in a launch of their own; in the profiler). Copies are
 // bound by bytes.
 
 #include <string.h>
@@ -123,8 +127,8 @@ __device__ __forceinline__ int holder(const int32_t* upto, int n, int32_t r) {
   return lo;
 }
 
-// Slots and positions of the tokens t0, t0 + THREADS, ..: four, or (T up to kMany) all. A token's table entry is a trip to
-// memory, so four go out together.
+// Slots and positions of the four tokens t0, t0 + THREADS, .. (of all tokens where pages are taken, T up to 4 * kMost). A
+// token's table entry is a trip to memory, so the four go out together.
 template <int THREADS>
 __device__ __forceinline__ void list_tokens(const TakeParams& p, const int32_t* rows, const int32_t* length, const int32_t* first,
                                             const int32_t* tokens, int64_t all, int64_t t0) {
@@ -454,6 +458,8 @@ struct CopyParams {
 // EACH: vectors of a thread. Pages are read as they are (forks read the same one several times: 64 of 16 pages 9.6 us,
 // 13.8 with loads past the caches) and written past the caches (980 of 2048 pages of 32 KiB in four layers, 258 MB, with the
 // list's launches 59.4 us, 66.3 with stores into them). A workgroup for each pair: 51.7 of those 59.4, 5.7 TB/s the copy.
+// 4-bit pages, half of whose pools are exponents, a sixteenth of the codes: 980 of 8 heads of 128 in four layers, 137 MB, 22.1
+// us, 6.2 TB/s; 64, 9 MB, 3.2.
 template <class U, int EACH>
 __global__ __launch_bounds__(kCopyThreads) void qkn_pages_copy_kernel(const CopyParams p) {
   const CopyPool& c = p.pool[blockIdx.y];

@@ -14,10 +14,13 @@
 // gamma in registers was no faster than that: 35 to 48 us, 139 to 181.
 //
 // A 4-bit cache's blocks are four lanes' groups (where pairs are apart) or two lanes' both groups: the largest magnitude
-// crosses lanes by DPP, as integers, and the exponent is a carry from the mantissa. Rows that no vector fits, and heads that
-// do not put a block on neighbouring lanes, take half a wavefront for a block of 32. 8192 tokens of 16 + 4 + 4 heads, 88 MB,
-// 23.0 us: 247 vector instructions a wavefront, issued for 10 of them; two tokens a wavefront, which share gamma, were
-// slower (25.4 for 24.4 at that time).
+// crosses lanes by DPP, as integers, and the exponent is a carry from the mantissa. Rows that no vector fits take half a
+// wavefront for a block of 32, and so do heads for whose rotation this is not written: pairs apart where head or rotation is
+// no multiple of 64, neighbouring pairs where the rotation is no multiple of 32. (Of rotations of 16 and 32 elements, and of
+// neighbouring pairs, blocks would be two lanes' both groups as well.) V goes with K there. 8192 tokens of 16 + 4 heads, 88 MB,
+// 23.0 us with two ranks: 247 vector instructions a wavefront, issued for 10 of them; two tokens a wavefront, which share
+// gamma, were slower (25.4 for 24.4 at that time). Element by element, 32 of each head rotated: 75.9 (vectors, 64 or all
+// rotated, 19 in calls in a row); 16 + 8 heads of 32, 16 rotated, 27 MB, 36.1 (none rotated 9.4).
 // Instructions count beside the bytes, so what would only move registers is not there: a kernel for each layout of pairs,
 // rows and slots addressed for all lanes at once, and lanes without gamma multiplied by 1 (16 + 4 + 4 heads over 4 bits, 354 ->
 // 247 vector instructions a wavefront, 24.4 -> 23.0 us; the cases below 24.5 -> 23.2, 70.7 -> 70.2, 5.4 -> 4.5).
