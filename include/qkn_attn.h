@@ -99,8 +99,8 @@ int64_t qkn_attn_workspace_bytes(const qkn_attn_args* args, const qkn_cache* cac
  * pools where T > 0; a workspace that is NULL or too small where one is needed.
  * QKN_ENOTSUP: head_dim over 256 or not a multiple of 8 (FP8: 16); page_size
  * below 16; q, out, pools, their strides not multiples of 16 bytes (q, out: 8
- * elements), workspace not 16-byte aligned; T * n_q, a page's bytes, or the
- * grid beyond 2^31.
+ * elements), workspace not 16-byte aligned; T * n_q or a page's bytes beyond
+ * 2^31, a grid's threads beyond 2^32.
  * QKN_EOVERLAP: an output (out, lse, workspace) overlapping an input or
  * another output.
  */
